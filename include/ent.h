@@ -319,6 +319,109 @@ int ent_decode_step_append(ent_ctx* c, int B, const float* logits, long long ld,
                            float* row_stats, int* kept, int* n_kept, float* out, float* lse,
                            int* tokens, float* scores, float* theta, void* stream);
 
+/* ---- Prompts: packed rows, their place in the cache, attention over them ----
+ *
+ * A batch of requests is packed: the tokens of request 0, then of request 1,
+ * and so on, one row each; starts (int [B + 1]) holds where each begins, and
+ * starts[B] their number.  Arrays may be longer (T, max_tokens rows): rows from
+ * starts[B] on are padding, which is neither read as a request's nor written.
+ * Calls take at most ENT_MAX_PACKED_TOKENS rows (else ENT_E_UNSUPPORTED).
+ * Row strides (ld*, in elements) let the queries, keys and values be parts of
+ * one projection's rows; the H d values of a row are contiguous.  Strides are
+ * whole multiples of 16 bytes, pointers 16-byte aligned. */
+#define ENT_MAX_PACKED_TOKENS (1 << 21)
+
+/* The place of a batch's new tokens: request b holds ctx_lens[b] tokens (0 for
+ * a new prompt) and gets n_new[b] more (1 for every sequence makes room for a
+ * decode step's append).  Blocks that it lacks, ceil((ctx + n) / 16) -
+ * ceil(ctx / 16), come from the free list free_ids[free_range[0] ..
+ * free_range[1]) in order, request 0's first; free_range (device int [2], at
+ * most n_ids) is moved past them.  Requests are served in order: the first that
+ * the free list or max_tokens has no room for, and all behind it, get nothing
+ * (their tokens count 0, ENT_DEV_CACHE_FULL).
+ *   starts[b]     = tokens that the requests before b got
+ *   block_tables  : entries of the new blocks written, the others left alone
+ *   slots[t]      = 16 * (physical block) + slot of packed token t; -1 from
+ *                   starts[B] to max_tokens (long long [max_tokens])
+ *   new_lens[b]   = ctx_lens[b] + the tokens that b got (nullable; for a step's
+ *                   growth leave it out, as ent_kv_append counts by itself)
+ * A request that is out of range (negative, or past max_blocks_per_seq blocks)
+ * gets nothing and raises ENT_DEV_BAD_CTXLEN or ENT_DEV_CACHE_FULL; a free id or
+ * a table entry outside the pool gives slot -1 (and table entry -1) and raises
+ * ENT_DEV_BAD_TABLE, as does a free_range outside [0, n_ids], which serves none.
+ * free_ids must name each block once and none in use.  new_lens must not alias
+ * n_new or ctx_lens. */
+int ent_prompt_plan(ent_ctx* c, int B, const int* n_new, const int* ctx_lens, int* block_tables,
+                    const int* free_ids, int n_ids, int* free_range, int max_tokens, int* starts,
+                    long long* slots, int* new_lens, void* stream);
+
+/* Keys and values of T packed tokens into the cache (the append of many tokens
+ * at once): token t's row k[t * ldk ..] (H_kv * d values, kv_dtype) to k_cache at
+ * slot slots[t], v to v_cache; a slot of -1 skips the token, one outside the
+ * pool too (ENT_DEV_BAD_TABLE).  ksum[p, g, :] of every block written becomes
+ * the mean over its slots 0 .. the last written one, as ent_block_summary gives
+ * it, bit for bit (nullable in the exact scoring mode).  The tokens of one block
+ * must be consecutive rows in slot order, as ent_prompt_plan lays them out, and
+ * the slots before them already hold tokens.  Context lengths are the caller's
+ * (new_lens of the plan). */
+int ent_prompt_store(ent_ctx* c, int T, const void* k, long long ldk, const void* v, long long ldv,
+                     const long long* slots, void* k_cache, void* v_cache, float* ksum,
+                     void* stream);
+
+/* Causal attention over B packed prompts: for token t of the request that
+ * begins at s, and query head h (KV head g = h / G), over u = s .. t
+ *   out[t, h, :] = sum_u softmax(scale <q_th, k_ug>)_u v_ug,
+ *   lse[t, h] = ln sum_u e^(scale <q_th, k_ug>)
+ * q, k, v: kv_dtype, T rows of H_q d, H_kv d and H_kv d values with strides ldq,
+ * ldk, ldv; out: kv_dtype, stride ldo >= H_q d, rounded once from 32 bits; lse
+ * (nullable): float [T, H_q].  With bf16 the weights are rounded to bf16 for the
+ * product with V (their sum is not).  Keys and values outside a row's range do
+ * not touch it, whatever they hold.  starts: int [B + 1], ascending from 0 to at
+ * most T (empty requests allowed); rows from starts[B] on are left as they are.
+ * The paged cache is not read: num_pool_blocks and max_blocks_per_seq do not
+ * matter here.  out must not overlap q, k or v. */
+int ent_prompt_attention(ent_ctx* c, int B, int T, const void* q, long long ldq, const void* k,
+                         long long ldk, const void* v, long long ldv, const int* starts, void* out,
+                         long long ldo, float* lse, void* stream);
+
+/* ---- A paged cache in 8 bits ----
+ *
+ * k_cache and v_cache as above, with e4m3 codes (one byte: OCP, no infinities,
+ * largest value 448) in place of the elements, and k_scale, v_scale: float
+ * [P, H_kv], one factor per (block, KV head) tile: key = k_scale[p, g] * code.
+ * Queries and new tokens are bf16: the context's kv_dtype must be ENT_BF16, and
+ * its scoring mean-key (the exact mode reads keys of the context's type), else
+ * ENT_E_UNSUPPORTED.  A step on such a cache is made of the staged calls
+ * (ent_entropy_temperature, ent_block_select, ent_sparse_paged_decode_q8,
+ * ent_sample); ent_block_summary and the one-call steps read a cache of the
+ * context's type.
+ *
+ * Rounding: a tile that begins with these tokens gets the smallest scale 2^k, k
+ * >= -64, with 448 2^k no less than the largest finite magnitude among them; a
+ * tile that holds earlier tokens gets the larger of that and its old scale, and
+ * where it grows the old codes are rounded again (exactly, but for what then
+ * falls under 2^-6 2^k).  code = x / scale to nearest even (x times the rounded
+ * reciprocal where the old scale is kept and no power of two); infinities
+ * saturate, NaN stay.  Scales that a caller makes must be finite and > 0. */
+
+/* ent_prompt_store into an 8-bit cache.  ksum: means of the keys as the cache
+ * then holds them (scale * mean code). */
+int ent_prompt_store_q8(ent_ctx* c, int T, const void* k, long long ldk, const void* v,
+                        long long ldv, const long long* slots, void* k_cache, void* v_cache,
+                        float* k_scale, float* v_scale, float* ksum, void* stream);
+
+/* ent_kv_append into an 8-bit cache (k_new, v_new: bf16 [B, H_kv, d], 16-byte
+ * aligned); ksum as in ent_prompt_store_q8. */
+int ent_kv_append_q8(ent_ctx* c, int B, const void* k_new, const void* v_new,
+                     const int* block_tables, int* ctx_lens, void* k_cache, void* v_cache,
+                     float* k_scale, float* v_scale, float* ksum, void* stream);
+
+/* ent_sparse_paged_decode over an 8-bit cache. */
+int ent_sparse_paged_decode_q8(ent_ctx* c, int B, const void* q, const void* k_cache,
+                               const void* v_cache, const float* k_scale, const float* v_scale,
+                               const int* block_tables, const int* ctx_lens, const int* kept,
+                               const int* n_kept, float* out, float* lse, void* stream);
+
 /* Entropy-aware scheduling over a pool of N active sequences (Section 3.1:
  * the priority pi(s) = E[Delta H_s] / (alpha C_s + beta M_s + gamma L_s);
  * Section 7: nonnegative bounded terms, no starvation).  Readings: the

@@ -98,6 +98,42 @@ int check_batch(ent_ctx* c, int B) {
   return ENT_OK;
 }
 
+// Packed rows: their number, and strides of whole 16-byte pieces that hold a row.
+int check_rows(ent_ctx* c, const char* who, int T) {
+  if (int r = check_device(c)) return r;
+  if (T < 0) return fail(c, ENT_E_INVAL, std::string(who) + ": negative number of rows");
+  if (T > ENT_MAX_PACKED_TOKENS)
+    return fail(c, ENT_E_UNSUPPORTED, std::string(who) + ": more than ENT_MAX_PACKED_TOKENS rows");
+  return ENT_OK;
+}
+bool row_stride_ok(const ent_ctx* c, long long ld, int heads) {
+  const int piece = c->cfg.kv_dtype == ENT_BF16 ? 8 : 4;
+  return ld >= static_cast<long long>(heads) * c->cfg.head_dim && ld % piece == 0;
+}
+
+// An 8-bit cache needs a bf16 context with mean-key scoring.
+int check_q8(ent_ctx* c, const char* who) {
+  if (c->cfg.kv_dtype != ENT_BF16)
+    return fail(c, ENT_E_UNSUPPORTED, std::string(who) + ": an 8-bit cache needs kv_dtype ENT_BF16");
+  if (c->cfg.scoring != ENT_SCORE_MEANKEY)
+    return fail(c, ENT_E_UNSUPPORTED, std::string(who) + ": an 8-bit cache has mean-key scoring only");
+  return ENT_OK;
+}
+
+// Arguments of ent_prompt_store and its 8-bit form (T > 0).
+int check_store(ent_ctx* c, const char* who, const void* k, long long ldk, const void* v,
+                long long ldv, const long long* slots, const void* k_cache, const void* v_cache,
+                const float* ksum) {
+  if (!k || !v || !slots || !k_cache || !v_cache || (!ksum && c->cfg.scoring != ENT_SCORE_EXACT))
+    return fail(c, ENT_E_INVAL, std::string(who) + ": NULL required pointer");
+  if (!row_stride_ok(c, ldk, c->cfg.num_kv_heads) || !row_stride_ok(c, ldv, c->cfg.num_kv_heads))
+    return fail(c, ENT_E_INVAL, std::string(who) + ": row strides need H_kv d elements or more, in 16-byte steps");
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
+      !aligned(slots, 8))
+    return fail(c, ENT_E_INVAL, std::string(who) + ": k, v and the caches need 16-byte alignment, slots 8");
+  return ENT_OK;
+}
+
 size_t align_up(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
@@ -449,6 +485,126 @@ int ent_kv_append(ent_ctx* c, int B, const void* k_new, const void* v_new, const
   const hipError_t e = ent::launch_kv_append(c, B, k_new, v_new, block_tables, ctx_lens, k_cache,
                                              v_cache, ksum, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(c, e, "ent_kv_append launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_prompt_plan(ent_ctx* c, int B, const int* n_new, const int* ctx_lens, int* block_tables,
+                    const int* free_ids, int n_ids, int* free_range, int max_tokens, int* starts,
+                    long long* slots, int* new_lens, void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_batch(c, B)) return r;
+  if (int r = check_rows(c, "ent_prompt_plan", max_tokens)) return r;
+  if (n_ids < 0) return fail(c, ENT_E_INVAL, "ent_prompt_plan: n_ids must be >= 0");
+  if (B == 0) return ENT_OK;
+  if (!n_new || !ctx_lens || !block_tables || (!free_ids && n_ids > 0) || !free_range || !starts ||
+      (!slots && max_tokens > 0))
+    return fail(c, ENT_E_INVAL, "ent_prompt_plan: NULL required pointer");
+  if (new_lens && (new_lens == n_new || new_lens == ctx_lens))
+    return fail(c, ENT_E_INVAL, "ent_prompt_plan: new_lens aliases n_new or ctx_lens");
+  if (!aligned(slots, 8)) return fail(c, ENT_E_INVAL, "ent_prompt_plan: slots needs 8-byte alignment");
+  const hipError_t e = ent::launch_prompt_plan(c, B, n_new, ctx_lens, block_tables, free_ids, n_ids,
+                                               free_range, max_tokens, starts, slots, new_lens,
+                                               static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(c, e, "ent_prompt_plan launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_prompt_store(ent_ctx* c, int T, const void* k, long long ldk, const void* v, long long ldv,
+                     const long long* slots, void* k_cache, void* v_cache, float* ksum,
+                     void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_rows(c, "ent_prompt_store", T)) return r;
+  if (T == 0) return ENT_OK;
+  if (int r = check_store(c, "ent_prompt_store", k, ldk, v, ldv, slots, k_cache, v_cache, ksum))
+    return r;
+  const hipError_t e = ent::launch_prompt_store(c, T, k, ldk, v, ldv, slots, k_cache, v_cache, ksum,
+                                                static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(c, e, "ent_prompt_store launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_prompt_store_q8(ent_ctx* c, int T, const void* k, long long ldk, const void* v,
+                        long long ldv, const long long* slots, void* k_cache, void* v_cache,
+                        float* k_scale, float* v_scale, float* ksum, void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_rows(c, "ent_prompt_store_q8", T)) return r;
+  if (int r = check_q8(c, "ent_prompt_store_q8")) return r;
+  if (T == 0) return ENT_OK;
+  if (int r = check_store(c, "ent_prompt_store_q8", k, ldk, v, ldv, slots, k_cache, v_cache, ksum))
+    return r;
+  if (!k_scale || !v_scale) return fail(c, ENT_E_INVAL, "ent_prompt_store_q8: NULL required pointer");
+  const hipError_t e = ent::launch_prompt_store_q8(c, T, k, ldk, v, ldv, slots, k_cache, v_cache,
+                                                   k_scale, v_scale, ksum,
+                                                   static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(c, e, "ent_prompt_store_q8 launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_prompt_attention(ent_ctx* c, int B, int T, const void* q, long long ldq, const void* k,
+                         long long ldk, const void* v, long long ldv, const int* starts, void* out,
+                         long long ldo, float* lse, void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_batch(c, B)) return r;
+  if (int r = check_rows(c, "ent_prompt_attention", T)) return r;
+  if (B == 0 || T == 0) return ENT_OK;
+  if (!q || !k || !v || !starts || !out)
+    return fail(c, ENT_E_INVAL, "ent_prompt_attention: NULL required pointer");
+  const int Hq = c->cfg.num_q_heads, Hkv = c->cfg.num_kv_heads;
+  if (!row_stride_ok(c, ldq, Hq) || !row_stride_ok(c, ldo, Hq) || !row_stride_ok(c, ldk, Hkv) ||
+      !row_stride_ok(c, ldv, Hkv))
+    return fail(c, ENT_E_INVAL,
+                "ent_prompt_attention: row strides need the row's elements or more, in 16-byte steps");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16))
+    return fail(c, ENT_E_INVAL, "ent_prompt_attention: q, k, v and out need 16-byte alignment");
+  const hipError_t e = ent::launch_prompt_attention(c, B, T, q, ldq, k, ldk, v, ldv, starts, out, ldo,
+                                                    lse, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(c, e, "ent_prompt_attention launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_kv_append_q8(ent_ctx* c, int B, const void* k_new, const void* v_new,
+                     const int* block_tables, int* ctx_lens, void* k_cache, void* v_cache,
+                     float* k_scale, float* v_scale, float* ksum, void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_batch(c, B)) return r;
+  if (int r = check_q8(c, "ent_kv_append_q8")) return r;
+  if (B == 0) return ENT_OK;
+  if (!k_new || !v_new || !block_tables || !ctx_lens || !k_cache || !v_cache || !k_scale || !v_scale ||
+      !ksum)
+    return fail(c, ENT_E_INVAL, "ent_kv_append_q8: NULL required pointer");
+  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16))
+    return fail(c, ENT_E_INVAL, "ent_kv_append_q8: k_new, v_new and the caches need 16-byte alignment");
+  const hipError_t e = ent::launch_kv_append_q8(c, B, k_new, v_new, block_tables, ctx_lens, k_cache,
+                                                v_cache, k_scale, v_scale, ksum,
+                                                static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(c, e, "ent_kv_append_q8 launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_sparse_paged_decode_q8(ent_ctx* c, int B, const void* q, const void* k_cache,
+                               const void* v_cache, const float* k_scale, const float* v_scale,
+                               const int* block_tables, const int* ctx_lens, const int* kept,
+                               const int* n_kept, float* out, float* lse, void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_batch(c, B)) return r;
+  if (int r = check_q8(c, "ent_sparse_paged_decode_q8")) return r;
+  if (B == 0) return ENT_OK;
+  if (!q || !k_cache || !v_cache || !k_scale || !v_scale || !block_tables || !ctx_lens || !kept ||
+      !n_kept || !out)
+    return fail(c, ENT_E_INVAL, "ent_sparse_paged_decode_q8: NULL required pointer");
+  if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16))
+    return fail(c, ENT_E_INVAL,
+                "ent_sparse_paged_decode_q8: q, caches and out need 16-byte alignment");
+  const hipError_t e = ent::launch_decode(c, B, q, k_cache, v_cache, block_tables, ctx_lens, kept,
+                                          n_kept, out, lse, static_cast<hipStream_t>(stream), nullptr,
+                                          nullptr, nullptr, k_scale, v_scale);
+  if (e != hipSuccess) return hip_fail(c, e, "ent_sparse_paged_decode_q8 launch");
   c->err.clear();
   return ENT_OK;
 }

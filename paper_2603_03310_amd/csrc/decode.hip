@@ -58,6 +58,8 @@ struct DecodeArgs {
   const void* q;
   const void* kc;
   const void* vc;
+  const float* ks;    // [P, H_kv] scales of an 8-bit cache
+  const float* vs;
   const int* tables;
   const int* ctx_lens;
   const int* kept;
@@ -258,6 +260,188 @@ __device__ __forceinline__ s16x4_t load_s16x4(const uint16_t* p) {
   return __builtin_bit_cast(s16x4_t, x);
 }
 
+constexpr int kSlots = 2 * kWaves;           // cut partials of a workgroup
+
+// The sums of a wave's segment, in the accumulator layout (lane (head r16, gq):
+// dims 16 m + 4 gq .. + 3): to the outputs where its range [u0, u1) holds the
+// whole segment, else to the wave's slot of the workgroup merge.
+template <int D>
+__device__ __forceinline__ void flush_segment(const DecodeArgs& a, int cur_seg, float m_run,
+                                              float l_run, const f32x4_t (&oacc)[D / 16], int u0,
+                                              int u1, const int* s_pref, const int* s_nk,
+                                              float* s_cacc, float* s_cml, int* s_cseg) {
+  constexpr int MT = D / 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int r16 = lane & 15, gq = lane >> 4;
+  const int G = a.G, Hq = a.Hkv * G;
+  const bool head_ok = r16 < G;
+  const float l_tot = xor_add<32>(xor_add<16>(l_run));
+  const int b = cur_seg / a.Hkv, g = cur_seg % a.Hkv;
+  const int seg_start = s_pref[b] + g * s_nk[b];
+  const int seg_end = seg_start + s_nk[b];
+  if (!head_ok) return;
+  if (seg_start >= u0 && seg_end <= u1) {
+    const long long oh = static_cast<long long>(b) * Hq + g * G + r16;
+    const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const f32x4_t o = oacc[m] * inv;
+      *reinterpret_cast<float4*>(a.out + oh * D + 16 * m + 4 * gq) = make_float4(o[0], o[1], o[2], o[3]);
+    }
+    if (gq == 0 && a.lse) a.lse[oh] = l_tot > 0.f ? (m_run + log2f(l_tot)) * kLn2 : -INFINITY;
+  } else {
+    // Cut by this wave's range: keep the partial for the workgroup merge.
+    const int cs = 2 * wave + (seg_start < u0 ? 0 : 1);
+    if (lane == 0) s_cseg[cs] = cur_seg;
+    float* acc = s_cacc + (static_cast<long long>(cs) * G + r16) * D;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+      *reinterpret_cast<float4*>(acc + 16 * m + 4 * gq) =
+          make_float4(oacc[m][0], oacc[m][1], oacc[m][2], oacc[m][3]);
+    if (gq == 0) {
+      s_cml[(cs * kMaxGroup + r16) * 2 + 0] = m_run;
+      s_cml[(cs * kMaxGroup + r16) * 2 + 1] = l_tot;
+    }
+  }
+}
+
+// The end of a workgroup of the MFMA decodes: its waves' cut segments merged.
+// s_w: three floats per slot and head, free once every wave is here.
+template <int D>
+__device__ __forceinline__ void merge_workgroup(const DecodeArgs& a, int U, int R, const int* s_pref,
+                                                const int* s_nk, const float* s_cacc,
+                                                const float* s_cml, const int* s_cseg, int4* s_gd,
+                                                int& s_ng, float* s_w) {
+  const int G = a.G;
+  // Workgroup merge: consecutive slots of one segment (in unit order) are one
+  // group; a group whose segment lies inside the workgroup's range is final,
+  // else it becomes the workgroup's partial of that segment (slot wg + seg).
+  // First, per (slot, head), the slot's weight 2^(m - M) in its group and the
+  // group's (M, L), all slots' loads issued at once; then every output is one
+  // weighted sum over its group's slots, in slot order, four consecutive
+  // outputs per thread (16-byte LDS reads and stores: with one float each the
+  // stores, issued while the other workgroups' loads fill the CU's memory
+  // pipeline, made this loop the longest part of a workgroup's end).
+  static_assert(kSlots * kMaxGroup + kSlots <= kThreads, "one thread per (slot, head), then per slot");
+  float* s_wf = s_w;
+  float* s_wm = s_wf + kSlots * kMaxGroup;
+  float* s_wl = s_wm + kSlots * kMaxGroup;
+  __syncthreads();
+  if (threadIdx.x < kSlots * kMaxGroup) {
+    const int k = threadIdx.x / kMaxGroup, r = threadIdx.x % kMaxGroup;
+    const int seg = s_cseg[k];
+    float f = 0.f, M = -INFINITY, L = 0.f;
+    if (seg >= 0 && r < G) {
+#pragma unroll
+      for (int kk = 0; kk < kSlots; ++kk)
+        if (s_cseg[kk] == seg && s_cml[(kk * kMaxGroup + r) * 2 + 1] > 0.f)
+          M = fmaxf(M, s_cml[(kk * kMaxGroup + r) * 2]);
+#pragma unroll
+      for (int kk = 0; kk < kSlots; ++kk) {
+        const float l = s_cml[(kk * kMaxGroup + r) * 2 + 1];
+        if (s_cseg[kk] != seg || !(l > 0.f)) continue;
+        const float fk = exp2f(s_cml[(kk * kMaxGroup + r) * 2] - M);
+        L += l * fk;
+        if (kk == k) f = fk;
+      }
+    }
+    s_wf[threadIdx.x] = f;
+    s_wm[threadIdx.x] = M;
+    s_wl[threadIdx.x] = L;
+  } else if (threadIdx.x < kSlots * kMaxGroup + kSlots) {
+    // Meanwhile, one thread per slot: a slot heads a group when it holds a
+    // segment other than that of the nearest earlier slot holding one; the
+    // group runs to the next slot holding another segment (the empty slots
+    // between weigh 0).  The heads, in slot order, get the group's slots,
+    // whether the segment lies inside this workgroup's range, and the record
+    // of a cut segment that begins in it.
+    const int k = threadIdx.x - kSlots * kMaxGroup;
+    int cs[kSlots];
+#pragma unroll
+    for (int kk = 0; kk < kSlots; ++kk) cs[kk] = s_cseg[kk];
+    bool hd[kSlots];
+    int prev = -1;
+#pragma unroll
+    for (int kk = 0; kk < kSlots; ++kk) {
+      hd[kk] = cs[kk] >= 0 && cs[kk] != prev;
+      if (cs[kk] >= 0) prev = cs[kk];
+    }
+    int seg = -1, rank = 0, ng = 0;
+    bool head = false;
+#pragma unroll
+    for (int kk = 0; kk < kSlots; ++kk) {
+      if (kk == k) {
+        seg = cs[kk];
+        head = hd[kk];
+      }
+      if (kk < k && hd[kk]) ++rank;
+      if (hd[kk]) ++ng;
+    }
+    int j = kSlots;
+#pragma unroll
+    for (int kk = kSlots - 1; kk >= 0; --kk)
+      if (kk > k && cs[kk] >= 0 && cs[kk] != seg) j = kk;
+    if (head) {
+      const int b = seg / a.Hkv, g = seg % a.Hkv;
+      const int seg_start = s_pref[b] + g * s_nk[b];
+      const int seg_end = seg_start + s_nk[b];
+      const int wg = blockIdx.x;
+      const int g0 = wg_begin(wg, U, R), g1 = wg_begin(wg + 1, U, R);
+      const bool whole = seg_start >= g0 && seg_end <= g1;
+      const bool own = !whole && seg_start >= g0;
+      s_gd[rank] = make_int4(k | (j << 8) | (whole ? 1 << 16 : 0) | (own ? 1 << 17 : 0), seg,
+                             own ? wg_of(seg_end - 1, U, R) : 0, 0);
+    }
+    if (k == 0) s_ng = ng;
+  }
+  __syncthreads();
+  const int wg = blockIdx.x;
+  int owner = -1, owner_last = 0;            // cut segment that begins in this range
+  const int ng = s_ng;
+  for (int gi = 0; gi < ng; ++gi) {
+    const int4 gd = s_gd[gi];
+    // Slots i .. j-1 with s_cseg == seg form the group (the others weigh 0).
+    const int i = gd.x & 255, j = (gd.x >> 8) & 255;
+    const bool whole = (gd.x >> 16) & 1;
+    const int seg = gd.y;
+    const long long slot = static_cast<long long>(wg) + seg;
+    if ((gd.x >> 17) & 1) {
+      owner = seg;
+      owner_last = gd.z;
+    }
+    for (int o = threadIdx.x; o < G * D / 4; o += kThreads) {
+      const int r = (4 * o) / D, d = 4 * o - r * D;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kSlots; ++k) {
+        const float f = s_wf[k * kMaxGroup + r];
+        const float4 v = *reinterpret_cast<const float4*>(s_cacc + (k * G + r) * D + d);
+        if (k >= i && k < j && f != 0.f) {
+          acc.x += f * v.x;
+          acc.y += f * v.y;
+          acc.z += f * v.z;
+          acc.w += f * v.w;
+        }
+      }
+      const float M = s_wm[i * kMaxGroup + r], L = s_wl[i * kMaxGroup + r];
+      if (whole) {
+        const long long oh = static_cast<long long>(seg) * G + r;    // b H_q + g G + r
+        const float4 res = L > 0.f ? make_float4(acc.x / L, acc.y / L, acc.z / L, acc.w / L)
+                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+        *reinterpret_cast<float4*>(a.out + oh * D + d) = res;
+        if (d == 0 && a.lse) a.lse[oh] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+      } else {
+        *reinterpret_cast<float4*>(a.part_acc + (slot * G + r) * D + d) = acc;
+        if (d == 0) {
+          a.part_ml[(slot * G + r) * 2 + 0] = M;
+          a.part_ml[(slot * G + r) * 2 + 1] = L;
+        }
+      }
+    }
+  }
+  if (threadIdx.x == 0) a.rec[wg] = make_int2(owner, owner_last);
+}
+
 template <int D>
 __global__ __launch_bounds__(kThreads, 3) void decode_bf16_kernel(DecodeArgs a) {
   constexpr int KS = D / 32;      // QK k-steps (32 dims each)
@@ -345,34 +529,7 @@ __global__ __launch_bounds__(kThreads, 3) void decode_bf16_kernel(DecodeArgs a) 
   }
 
   auto flush = [&]() {
-    const float l_tot = xor_add<32>(xor_add<16>(l_run));
-    const int b = cur_seg / a.Hkv, g = cur_seg % a.Hkv;
-    const int seg_start = s_pref[b] + g * s_nk[b];
-    const int seg_end = seg_start + s_nk[b];
-    if (!head_ok) return;
-    if (seg_start >= u0 && seg_end <= u1) {
-      const long long oh = static_cast<long long>(b) * Hq + g * G + r16;
-      const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const f32x4_t o = oacc[m] * inv;
-        *reinterpret_cast<float4*>(a.out + oh * D + 16 * m + 4 * gq) = make_float4(o[0], o[1], o[2], o[3]);
-      }
-      if (gq == 0 && a.lse) a.lse[oh] = l_tot > 0.f ? (m_run + log2f(l_tot)) * kLn2 : -INFINITY;
-    } else {
-      // Cut by this wave's range: keep the partial for the workgroup merge.
-      const int cs = 2 * wave + (seg_start < u0 ? 0 : 1);
-      if (lane == 0) s_cseg[cs] = cur_seg;
-      float* acc = s_cacc + (static_cast<long long>(cs) * G + r16) * D;
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-        *reinterpret_cast<float4*>(acc + 16 * m + 4 * gq) =
-            make_float4(oacc[m][0], oacc[m][1], oacc[m][2], oacc[m][3]);
-      if (gq == 0) {
-        s_cml[(cs * kMaxGroup + r16) * 2 + 0] = m_run;
-        s_cml[(cs * kMaxGroup + r16) * 2 + 1] = l_tot;
-      }
-    }
+    flush_segment<D>(a, cur_seg, m_run, l_run, oacc, u0, u1, s_pref, s_nk, s_cacc, s_cml, s_cseg);
   };
 
   // One unit: compute on the tiles in (kc, vc) while the next unit's tiles
@@ -499,138 +656,239 @@ __global__ __launch_bounds__(kThreads, 3) void decode_bf16_kernel(DecodeArgs a) 
   }
   if (busy) flush();
 
-  // Workgroup merge: consecutive slots of one segment (in unit order) are one
-  // group; a group whose segment lies inside the workgroup's range is final,
-  // else it becomes the workgroup's partial of that segment (slot wg + seg).
-  // First, per (slot, head), the slot's weight 2^(m - M) in its group and the
-  // group's (M, L), all slots' loads issued at once; then every output is one
-  // weighted sum over its group's slots, in slot order, four consecutive
-  // outputs per thread (16-byte LDS reads and stores: with one float each the
-  // stores, issued while the other workgroups' loads fill the CU's memory
-  // pipeline, made this loop the longest part of a workgroup's end).
-  constexpr int kSlots = 2 * kWaves;
-  static_assert(kSlots * kMaxGroup + kSlots <= kThreads, "one thread per (slot, head), then per slot");
-  static_assert(3 * kSlots * kMaxGroup * sizeof(float) <= sizeof(s_kst), "merge weights in the K rows");
   // The K staging rows are dead once every wave has left its loop.
-  float* s_wf = reinterpret_cast<float*>(s_kst);
-  float* s_wm = s_wf + kSlots * kMaxGroup;
-  float* s_wl = s_wm + kSlots * kMaxGroup;
-  __syncthreads();
-  if (threadIdx.x < kSlots * kMaxGroup) {
-    const int k = threadIdx.x / kMaxGroup, r = threadIdx.x % kMaxGroup;
-    const int seg = s_cseg[k];
-    float f = 0.f, M = -INFINITY, L = 0.f;
-    if (seg >= 0 && r < G) {
-#pragma unroll
-      for (int kk = 0; kk < kSlots; ++kk)
-        if (s_cseg[kk] == seg && s_cml[(kk * kMaxGroup + r) * 2 + 1] > 0.f)
-          M = fmaxf(M, s_cml[(kk * kMaxGroup + r) * 2]);
-#pragma unroll
-      for (int kk = 0; kk < kSlots; ++kk) {
-        const float l = s_cml[(kk * kMaxGroup + r) * 2 + 1];
-        if (s_cseg[kk] != seg || !(l > 0.f)) continue;
-        const float fk = exp2f(s_cml[(kk * kMaxGroup + r) * 2] - M);
-        L += l * fk;
-        if (kk == k) f = fk;
-      }
-    }
-    s_wf[threadIdx.x] = f;
-    s_wm[threadIdx.x] = M;
-    s_wl[threadIdx.x] = L;
-  } else if (threadIdx.x < kSlots * kMaxGroup + kSlots) {
-    // Meanwhile, one thread per slot: a slot heads a group when it holds a
-    // segment other than that of the nearest earlier slot holding one; the
-    // group runs to the next slot holding another segment (the empty slots
-    // between weigh 0).  The heads, in slot order, get the group's slots,
-    // whether the segment lies inside this workgroup's range, and the record
-    // of a cut segment that begins in it.
-    const int k = threadIdx.x - kSlots * kMaxGroup;
-    int cs[kSlots];
-#pragma unroll
-    for (int kk = 0; kk < kSlots; ++kk) cs[kk] = s_cseg[kk];
-    bool hd[kSlots];
-    int prev = -1;
-#pragma unroll
-    for (int kk = 0; kk < kSlots; ++kk) {
-      hd[kk] = cs[kk] >= 0 && cs[kk] != prev;
-      if (cs[kk] >= 0) prev = cs[kk];
-    }
-    int seg = -1, rank = 0, ng = 0;
-    bool head = false;
-#pragma unroll
-    for (int kk = 0; kk < kSlots; ++kk) {
-      if (kk == k) {
-        seg = cs[kk];
-        head = hd[kk];
-      }
-      if (kk < k && hd[kk]) ++rank;
-      if (hd[kk]) ++ng;
-    }
-    int j = kSlots;
-#pragma unroll
-    for (int kk = kSlots - 1; kk >= 0; --kk)
-      if (kk > k && cs[kk] >= 0 && cs[kk] != seg) j = kk;
-    if (head) {
-      const int b = seg / a.Hkv, g = seg % a.Hkv;
-      const int seg_start = s_pref[b] + g * s_nk[b];
-      const int seg_end = seg_start + s_nk[b];
-      const int wg = blockIdx.x;
-      const int g0 = wg_begin(wg, U, R), g1 = wg_begin(wg + 1, U, R);
-      const bool whole = seg_start >= g0 && seg_end <= g1;
-      const bool own = !whole && seg_start >= g0;
-      s_gd[rank] = make_int4(k | (j << 8) | (whole ? 1 << 16 : 0) | (own ? 1 << 17 : 0), seg,
-                             own ? wg_of(seg_end - 1, U, R) : 0, 0);
-    }
-    if (k == 0) s_ng = ng;
-  }
-  __syncthreads();
-  const int wg = blockIdx.x;
-  int owner = -1, owner_last = 0;            // cut segment that begins in this range
-  const int ng = s_ng;
-  for (int gi = 0; gi < ng; ++gi) {
-    const int4 gd = s_gd[gi];
-    // Slots i .. j-1 with s_cseg == seg form the group (the others weigh 0).
-    const int i = gd.x & 255, j = (gd.x >> 8) & 255;
-    const bool whole = (gd.x >> 16) & 1;
-    const int seg = gd.y;
-    const long long slot = static_cast<long long>(wg) + seg;
-    if ((gd.x >> 17) & 1) {
-      owner = seg;
-      owner_last = gd.z;
-    }
-    for (int o = threadIdx.x; o < G * D / 4; o += kThreads) {
-      const int r = (4 * o) / D, d = 4 * o - r * D;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < kSlots; ++k) {
-        const float f = s_wf[k * kMaxGroup + r];
-        const float4 v = *reinterpret_cast<const float4*>(s_cacc + (k * G + r) * D + d);
-        if (k >= i && k < j && f != 0.f) {
-          acc.x += f * v.x;
-          acc.y += f * v.y;
-          acc.z += f * v.z;
-          acc.w += f * v.w;
-        }
-      }
-      const float M = s_wm[i * kMaxGroup + r], L = s_wl[i * kMaxGroup + r];
-      if (whole) {
-        const long long oh = static_cast<long long>(seg) * G + r;    // b H_q + g G + r
-        const float4 res = L > 0.f ? make_float4(acc.x / L, acc.y / L, acc.z / L, acc.w / L)
-                                   : make_float4(0.f, 0.f, 0.f, 0.f);
-        *reinterpret_cast<float4*>(a.out + oh * D + d) = res;
-        if (d == 0 && a.lse) a.lse[oh] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
-      } else {
-        *reinterpret_cast<float4*>(a.part_acc + (slot * G + r) * D + d) = acc;
-        if (d == 0) {
-          a.part_ml[(slot * G + r) * 2 + 0] = M;
-          a.part_ml[(slot * G + r) * 2 + 1] = L;
-        }
-      }
-    }
-  }
-  if (threadIdx.x == 0) a.rec[wg] = make_int2(owner, owner_last);
+  static_assert(3 * kSlots * kMaxGroup * sizeof(float) <= sizeof(s_kst), "merge weights in the K rows");
+  merge_workgroup<D>(a, U, R, s_pref, s_nk, s_cacc, s_cml, s_cseg, s_gd, s_ng,
+                     reinterpret_cast<float*>(s_kst));
 }
 
+// 8-bit caches: e4m3 codes with a scale per (block, KV head).  The same ranges,
+// segments and merge; four units of a segment (64 tokens) go through the matrix
+// cores together, so that every lane loads 16 B pieces straight into the MFMA
+// layouts: lane (r16, gq) is row r16 of K tile t, taken to be token 4 t + r16 % 4
+// of block r16 / 4, so accumulator (gq, e) of tile t is token 4 t + e of block gq
+// and a lane's 16 scores are its block's 16 tokens; its V operand is the 16
+// tokens of one dim of the same block, one 16 B row of the dim-major tile.  The
+// scales are then one factor per lane: of its scores, and of its weights before
+// they are split.  The codes convert to bf16 exactly (4 significant bits), and
+// the weights go in as three bf16 parts (24 bits: the loads leave the matrix
+// cores idle), so the products are those of fp32.
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void decode_q8_kernel(DecodeArgs a) {
+  constexpr int KL = D / 64;      // 16 B pieces of a lane's part of a K row
+  constexpr int KS = D / 32;      // QK steps
+  constexpr int MT = D / 16;      // output tiles
+  constexpr int BL = 4;           // blocks of a group
+  extern __shared__ __attribute__((aligned(16))) int s_mem[];
+  __shared__ int s_red[kWaves];
+  __shared__ int s_cseg[kSlots];
+  __shared__ int4 s_gd[kSlots];
+  __shared__ int s_ng;
+  __shared__ float s_w[3 * kSlots * kMaxGroup];
+  float* s_cacc = reinterpret_cast<float*>(s_mem);
+  float* s_cml = s_cacc + kSlots * a.G * D;
+  int* s_pref = reinterpret_cast<int*>(s_cml + kSlots * kMaxGroup * 2);
+  int* s_nk = s_pref + a.B + 1;
+  int* s_N = s_nk + a.B;
+  build_plan(a, s_pref, s_nk, s_N, s_red);
+  const int U = s_pref[a.B];
+  const int lane = threadIdx.x & 63;
+  const int wave = threadIdx.x >> 6;
+  const int w = blockIdx.x * kWaves + wave;
+  zero_empty<D>(a, s_nk);
+  const int R = ranges_used(U, a.R, a.few);
+  if (U == 0 || blockIdx.x >= R) {
+    if (threadIdx.x == 0) a.rec[blockIdx.x] = make_int2(-1, 0);
+    return;
+  }
+  if (lane < 2) s_cseg[2 * wave + lane] = -1;
+  const int u0 = wv_begin(w, U, R), u1 = wv_begin(w + 1, U, R);
+  const int r16 = lane & 15, gq = lane >> 4;
+  const int Hq = a.Hkv * a.G;
+  const bool head_ok = r16 < a.G;
+  const uint16_t* q = static_cast<const uint16_t*>(a.q);
+  const unsigned char* kc = static_cast<const unsigned char*>(a.kc);
+  const unsigned char* vc = static_cast<const unsigned char*>(a.vc);
+
+  // 64 units of metadata, their scales with them.
+  int ubase = u0;
+  UnitMeta win{-1, -1, 0};
+  float wks = 0.f, wvs = 0.f;
+  auto window = [&](int u) {
+    ubase = u;
+    win = unit_meta(a, u + lane, u1, s_pref, s_nk, s_N);
+    wks = wvs = 0.f;
+    if (win.p >= 0) {
+      const long long x = static_cast<long long>(win.p) * a.Hkv + win.seg % a.Hkv;
+      wks = a.ks[x];
+      wvs = a.vs[x];
+    }
+  };
+  // Units from i on that make one group: at most four, of one segment.
+  auto group = [&](int i) {
+    const unsigned long long same = __ballot(win.seg == lane_at(win.seg, i)) >> i;
+    const int n = __builtin_ctzll(~same | (1ull << BL));
+    return n;
+  };
+  typedef u32x4_t Tiles[4 * KL + MT];      // K pieces, then V rows
+  auto load_tiles = [&](int i, int n, Tiles& x) {
+    const int g = max(lane_at(win.seg, i), 0) % a.Hkv;
+    const int pk = max(__shfl(win.p, i + min(r16 >> 2, n - 1)), 0);
+    const int pv = max(__shfl(win.p, i + min(gq, n - 1)), 0);
+    const unsigned char* kt = kc + (static_cast<long long>(pk) * a.Hkv + g) * kBlock * D +
+                              (r16 & 3) * D + gq * (D / 4);
+    const unsigned char* vt = vc + (static_cast<long long>(pv) * a.Hkv + g) * kBlock * D + r16 * kBlock;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int y = 0; y < KL; ++y)
+        x[t * KL + y] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kt + 4 * t * D + 16 * y));
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+      x[4 * KL + m] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vt + 16 * m * kBlock));
+  };
+  // Eight codes (two words) as bf16.
+  auto widen = [](unsigned lo, unsigned hi) {
+    const bf16x2_t x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
+    const bf16x2_t x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+    const bf16x2_t x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
+    const bf16x2_t x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+    return __builtin_bit_cast(
+        bf16x8_t, make_uint4(__builtin_bit_cast(unsigned, x0), __builtin_bit_cast(unsigned, x1),
+                             __builtin_bit_cast(unsigned, x2), __builtin_bit_cast(unsigned, x3)));
+  };
+
+  int cur_seg = -1;
+  bf16x8_t qreg[KS];
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x4_t oacc[MT];
+  auto begin_segment = [&](int seg) {
+    cur_seg = seg;
+    const int b = seg / a.Hkv, g = seg % a.Hkv;
+    const long long qh = static_cast<long long>(b) * Hq + g * a.G + r16;
+    // Step ks of lane (., gq) is dims gq D / 4 + 8 ks .. + 7, as in its K pieces.
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (head_ok) qreg[ks] = load_bf16x8(q + qh * D + gq * (D / 4) + 8 * ks);
+      else qreg[ks] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
+    }
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) oacc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  };
+  auto flush = [&]() {
+    flush_segment<D>(a, cur_seg, m_run, l_run, oacc, u0, u1, s_pref, s_nk, s_cacc, s_cml, s_cseg);
+  };
+
+  int u = u0, i = 0, n = 0;       // the group: units u .. u + n - 1, window place i
+  // One group: computes on x while the next group's tiles load into y.
+  auto step = [&](Tiles& x, Tiles& y) {
+    const int seg = lane_at(win.seg, i);
+    if (seg != cur_seg) {
+      if (cur_seg >= 0) flush();
+      begin_segment(seg);
+    }
+    const int mine = i + min(gq, n - 1);
+    const int nv0 = __shfl(win.nv, mine), p0 = __shfl(win.p, mine);
+    const int nv = gq < n && p0 >= 0 ? nv0 : 0;
+    const float ksl = __shfl(wks, mine) * a.scale_log2;
+    const float vsl0 = __shfl(wvs, mine);
+    const float vsl = nv > 0 ? vsl0 : 0.f;
+    u += n;
+    const bool more = u < u1;
+    if (more) {
+      i += n;
+      if (i == kWindow) {
+        window(u);
+        i = 0;
+      }
+      n = group(i);
+      load_tiles(i, n, y);
+    }
+    if (__any(nv > 0)) {
+      f32x4_t sc[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        sc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4_t p = x[t * KL + ks / 2];
+          const bf16x8_t kf = ks % 2 ? widen(p[2], p[3]) : widen(p[0], p[1]);
+          sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qreg[ks], sc[t], 0, 0, 0);
+        }
+      }
+      float mloc = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sc[t][e] = (4 * t + e < nv) ? sc[t][e] * ksl : -INFINITY;
+          mloc = fmaxf(mloc, sc[t][e]);
+        }
+      if (__any(mloc > m_run)) {
+        const float m_new = fmaxf(m_run, xor_max<32>(xor_max<16>(mloc)));
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= alpha;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) oacc[m] *= alpha;
+        m_run = m_new;
+      }
+      // Weights, their sum, and three bf16 parts of each times V's scale.
+      bf16x8_t pp[3][2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        unsigned wd[3][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int t = 2 * s + k / 2, e = 2 * (k % 2);
+          f32x2_t pe = {__builtin_amdgcn_exp2f(sc[t][e] - m_run), __builtin_amdgcn_exp2f(sc[t][e + 1] - m_run)};
+          l_run += pe.x + pe.y;
+          pe *= vsl;
+#pragma unroll
+          for (int j = 0; j < 3; ++j) {
+            const bf16x2_t part = __builtin_convertvector(pe, bf16x2_t);
+            pe -= __builtin_convertvector(part, f32x2_t);
+            wd[j][k] = __builtin_bit_cast(unsigned, part);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          pp[j][s] = __builtin_bit_cast(bf16x8_t, make_uint4(wd[j][0], wd[j][1], wd[j][2], wd[j][3]));
+      }
+      // Codes of rows that hold no token may be anything, NaN too.
+      if (__any(nv < kBlock)) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int keep = min(max(nv - 4 * k, 0), 4);
+          const unsigned mask = keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
+#pragma unroll
+          for (int m = 0; m < MT; ++m) x[4 * KL + m][k] &= mask;
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const bf16x8_t vf = widen(x[4 * KL + m][2 * s], x[4 * KL + m][2 * s + 1]);
+#pragma unroll
+          for (int j = 0; j < 3; ++j)
+            oacc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[j][s], oacc[m], 0, 0, 0);
+        }
+    }
+    return more;
+  };
+  if (u0 < u1) {
+    Tiles xa, xb;
+    window(u0);
+    n = group(0);
+    load_tiles(0, n, xa);
+    while (step(xa, xb) && step(xb, xa)) {
+    }
+    flush();
+  }
+  merge_workgroup<D>(a, U, R, s_pref, s_nk, s_cacc, s_cml, s_cseg, s_gd, s_ng, s_w);
+}
 // fp32: lane (t16, dq) holds dims dq D / 4 .. of token t16's key (16-byte
 // loads), so a score is a quarter dot product per lane and two adds across
 // lanes, every lane ends with its token's score and forms one weight per head;
@@ -981,12 +1239,14 @@ hipError_t launch_decode(const ent_ctx* c, int B, const void* q, const void* k_c
                          const void* v_cache, const int* tables, const int* ctx_lens,
                          const int* kept, const int* n_kept, float* out, float* lse,
                          hipStream_t s, const int* kept_phys, const AppendArgs* ap,
-                         const SampleArgs* sp) {
+                         const SampleArgs* sp, const float* k_scale, const float* v_scale) {
   const ent_config& cf = c->cfg;
   DecodeArgs a;
   a.q = q;
   a.kc = k_cache;
   a.vc = v_cache;
+  a.ks = k_scale;
+  a.vs = v_scale;
   a.tables = tables;
   a.ctx_lens = ctx_lens;
   a.kept = kept;
@@ -1016,7 +1276,11 @@ hipError_t launch_decode(const ent_ctx* c, int B, const void* q, const void* k_c
   const dim3 grid(nwg);
   if (cf.kv_dtype == ENT_BF16) {
     const size_t lds16 = decode_lds_bytes(B, c->group, cf.head_dim);
-    if (cf.head_dim == 128)
+    if (k_scale && cf.head_dim == 128)
+      hipLaunchKernelGGL(decode_q8_kernel<128>, grid, dim3(kThreads), lds16, s, a);
+    else if (k_scale)
+      hipLaunchKernelGGL(decode_q8_kernel<64>, grid, dim3(kThreads), lds16, s, a);
+    else if (cf.head_dim == 128)
       hipLaunchKernelGGL(decode_bf16_kernel<128>, grid, dim3(kThreads), lds16, s, a);
     else
       hipLaunchKernelGGL(decode_bf16_kernel<64>, grid, dim3(kThreads), lds16, s, a);

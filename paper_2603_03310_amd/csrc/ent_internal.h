@@ -186,11 +186,13 @@ struct SampleArgs {
 // ap (nullable): an append of one token per sequence, and sp (nullable) the
 // sampling of every row, that share the launch merging the split attention
 // segments (none of the three reads what another writes).
+// k_scale, v_scale (both or none): the caches hold e4m3 codes with these scales.
 hipError_t launch_decode(const ent_ctx* c, int B, const void* q, const void* k_cache,
                          const void* v_cache, const int* tables, const int* ctx_lens,
                          const int* kept, const int* n_kept, float* out, float* lse,
                          hipStream_t s, const int* kept_phys = nullptr,
-                         const AppendArgs* ap = nullptr, const SampleArgs* sp = nullptr);
+                         const AppendArgs* ap = nullptr, const SampleArgs* sp = nullptr,
+                         const float* k_scale = nullptr, const float* v_scale = nullptr);
 hipError_t launch_decode_step(const ent_ctx* c, int B, const float* logits, long long ld,
                               ent_state st, const void* q, const void* k_cache,
                               const void* v_cache, const float* ksum, const int* tables,
@@ -207,6 +209,27 @@ hipError_t launch_kv_append(const ent_ctx* c, int B, const void* k_new, const vo
 hipError_t launch_schedule(int N, const ent_sched_params& p, const float* tau, const int* n_kept,
                            const int* ctx_lens, float* tau_last, float* gain, int* age, int b_sel,
                            int* selected, int* n_selected, float* priority, hipStream_t s);
+
+// Prompts into the cache, and the 8-bit caches' stores (prompt.hip).
+hipError_t launch_prompt_plan(const ent_ctx* c, int B, const int* n_new, const int* ctx_lens,
+                              int* tables, const int* free_ids, int n_ids, int* free_range,
+                              int max_tokens, int* starts, long long* slots, int* new_lens,
+                              hipStream_t s);
+hipError_t launch_prompt_store(const ent_ctx* c, int T, const void* k, long long ldk, const void* v,
+                               long long ldv, const long long* slots, void* k_cache, void* v_cache,
+                               float* ksum, hipStream_t s);
+hipError_t launch_prompt_store_q8(const ent_ctx* c, int T, const void* k, long long ldk,
+                                  const void* v, long long ldv, const long long* slots,
+                                  void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                                  float* ksum, hipStream_t s);
+hipError_t launch_kv_append_q8(const ent_ctx* c, int B, const void* k_new, const void* v_new,
+                               const int* tables, int* ctx_lens, void* k_cache, void* v_cache,
+                               float* k_scale, float* v_scale, float* ksum, hipStream_t s);
+// Causal attention over packed prompts (attend.hip).
+hipError_t launch_prompt_attention(const ent_ctx* c, int B, int T, const void* q, long long ldq,
+                                   const void* k, long long ldk, const void* v, long long ldv,
+                                   const int* starts, void* out, long long ldo, float* lse,
+                                   hipStream_t s);
 
 // Configuration check of ent_init (message, ENT_OK / ENT_E_INVAL /
 // ENT_E_UNSUPPORTED in *code), and the message ent_last_error(NULL) returns

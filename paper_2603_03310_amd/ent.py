@@ -28,7 +28,10 @@ EXPORTED = ("ent_default_config", "ent_check_config", "ent_row_stats_chunks", "e
             "ent_destroy", "ent_last_error", "ent_device_status", "ent_entropy_temperature",
             "ent_block_summary", "ent_block_select", "ent_sparse_paged_decode", "ent_sample",
             "ent_kv_append", "ent_decode_step", "ent_schedule", "ent_entropy_temperature_noalloc",
-            "ent_decode_step_append")
+            "ent_decode_step_append", "ent_prompt_plan", "ent_prompt_store",
+            "ent_prompt_store_q8", "ent_prompt_attention", "ent_kv_append_q8",
+            "ent_sparse_paged_decode_q8")
+ENT_MAX_PACKED_TOKENS = 1 << 21
 ENT_NOALLOC_SCRATCH_BYTES = 2 << 20
 ENT_SCHED_MAX_POOL = 8192
 
@@ -102,6 +105,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "ent_decode_step_append": (i, [vp, i, vp, ll, ent_state] + [vp] * 20),
         "ent_schedule": (i, [vp, i, ctypes.POINTER(ent_sched_params)] + [vp] * 6
                          + [i] + [vp] * 4),
+        "ent_prompt_plan": (i, [vp, i, vp, vp, vp, vp, i, vp, i, vp, vp, vp, vp]),
+        "ent_prompt_store": (i, [vp, i, vp, ll, vp, ll] + [vp] * 5),
+        "ent_prompt_store_q8": (i, [vp, i, vp, ll, vp, ll] + [vp] * 7),
+        "ent_prompt_attention": (i, [vp, i, i, vp, ll, vp, ll, vp, ll, vp, vp, ll, vp, vp]),
+        "ent_kv_append_q8": (i, [vp, i] + [vp] * 10),
+        "ent_sparse_paged_decode_q8": (i, [vp, i] + [vp] * 12),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -250,3 +259,43 @@ def ent_schedule(ctx, N, prm: ent_sched_params, tau, n_kept, ctx_lens, tau_last,
                                     ptr(ctx_lens), ptr(tau_last), ptr(gain), ptr(age), b_sel,
                                     ptr(selected), ptr(n_selected), ptr(priority),
                                     _stream(stream)))
+
+
+def ent_prompt_plan(ctx, B, n_new, ctx_lens, block_tables, free_ids, n_ids, free_range, max_tokens,
+                    starts, slots, new_lens=None, stream=None):
+    _check(ctx, load().ent_prompt_plan(ctx, B, ptr(n_new), ptr(ctx_lens), ptr(block_tables),
+                                       ptr(free_ids), n_ids, ptr(free_range), max_tokens,
+                                       ptr(starts), ptr(slots), ptr(new_lens), _stream(stream)))
+
+
+def ent_prompt_store(ctx, T, k, ldk, v, ldv, slots, k_cache, v_cache, ksum, stream=None):
+    _check(ctx, load().ent_prompt_store(ctx, T, ptr(k), ldk, ptr(v), ldv, ptr(slots), ptr(k_cache),
+                                        ptr(v_cache), ptr(ksum), _stream(stream)))
+
+
+def ent_prompt_store_q8(ctx, T, k, ldk, v, ldv, slots, k_cache, v_cache, k_scale, v_scale, ksum,
+                        stream=None):
+    _check(ctx, load().ent_prompt_store_q8(ctx, T, ptr(k), ldk, ptr(v), ldv, ptr(slots),
+                                           ptr(k_cache), ptr(v_cache), ptr(k_scale), ptr(v_scale),
+                                           ptr(ksum), _stream(stream)))
+
+
+def ent_prompt_attention(ctx, B, T, q, ldq, k, ldk, v, ldv, starts, out, ldo, lse=None,
+                         stream=None):
+    _check(ctx, load().ent_prompt_attention(ctx, B, T, ptr(q), ldq, ptr(k), ldk, ptr(v), ldv,
+                                            ptr(starts), ptr(out), ldo, ptr(lse), _stream(stream)))
+
+
+def ent_kv_append_q8(ctx, B, k_new, v_new, block_tables, ctx_lens, k_cache, v_cache, k_scale,
+                     v_scale, ksum, stream=None):
+    _check(ctx, load().ent_kv_append_q8(ctx, B, ptr(k_new), ptr(v_new), ptr(block_tables),
+                                        ptr(ctx_lens), ptr(k_cache), ptr(v_cache), ptr(k_scale),
+                                        ptr(v_scale), ptr(ksum), _stream(stream)))
+
+
+def ent_sparse_paged_decode_q8(ctx, B, q, k_cache, v_cache, k_scale, v_scale, block_tables,
+                               ctx_lens, kept, n_kept, out, lse=None, stream=None):
+    _check(ctx, load().ent_sparse_paged_decode_q8(ctx, B, ptr(q), ptr(k_cache), ptr(v_cache),
+                                                  ptr(k_scale), ptr(v_scale), ptr(block_tables),
+                                                  ptr(ctx_lens), ptr(kept), ptr(n_kept), ptr(out),
+                                                  ptr(lse), _stream(stream)))

@@ -19,7 +19,11 @@ class Decoder:
     """Owns one library context; `step` runs the whole decode step, either as
     ent_entropy_temperature -> ent_block_select -> ent_sparse_paged_decode ->
     ent_sample (fused=False) or as the single call ent_decode_step (fused=True,
-    the default); the two give bit-identical results."""
+    the default); the two give bit-identical results.  With k_scale and v_scale
+    the caches hold 8-bit codes: `step` then runs the four calls (with
+    ent_sparse_paged_decode_q8), `store` and `append` the 8-bit forms.  `plan`,
+    `store` and `prompt` bring a batch of packed prompts into the cache and attend
+    over them."""
 
     def __init__(self, **fields):
         self.cfg = make_config(**fields)
@@ -41,9 +45,10 @@ class Decoder:
 
     def step(self, B, *, logits, h_prev, tau, temp, q, k_cache, v_cache, block_tables, ctx_lens,
              ksum, uniforms, h, temp_used, row_stats, kept, n_kept, out, tokens, lse=None,
-             scores=None, theta=None, stream=None, fused=True, kappa=None):
+             scores=None, theta=None, stream=None, fused=True, kappa=None, k_scale=None,
+             v_scale=None):
         ld = logits.stride(0)
-        if fused:
+        if fused and k_scale is None:
             ent.ent_decode_step(self.ctx, B, logits, ld, h_prev, tau, temp, q, k_cache, v_cache,
                                 ksum, block_tables, ctx_lens, uniforms, h, temp_used, kept,
                                 n_kept, out, tokens, row_stats, lse, scores, theta, stream, kappa)
@@ -52,13 +57,42 @@ class Decoder:
                                     row_stats, stream)
         ent.ent_block_select(self.ctx, B, q, ksum, block_tables, ctx_lens, h, kept, n_kept,
                              scores, theta, stream, kappa, k_cache)
-        ent.ent_sparse_paged_decode(self.ctx, B, q, k_cache, v_cache, block_tables, ctx_lens,
-                                    kept, n_kept, out, lse, stream)
+        if k_scale is None:
+            ent.ent_sparse_paged_decode(self.ctx, B, q, k_cache, v_cache, block_tables, ctx_lens,
+                                        kept, n_kept, out, lse, stream)
+        else:
+            ent.ent_sparse_paged_decode_q8(self.ctx, B, q, k_cache, v_cache, k_scale, v_scale,
+                                           block_tables, ctx_lens, kept, n_kept, out, lse, stream)
         ent.ent_sample(self.ctx, B, logits, ld, row_stats, temp_used, uniforms, tokens, stream)
 
-    def append(self, B, k_new, v_new, block_tables, ctx_lens, k_cache, v_cache, ksum, stream=None):
-        ent.ent_kv_append(self.ctx, B, k_new, v_new, block_tables, ctx_lens, k_cache, v_cache,
-                          ksum, stream)
+    def append(self, B, k_new, v_new, block_tables, ctx_lens, k_cache, v_cache, ksum, stream=None,
+               k_scale=None, v_scale=None):
+        if k_scale is None:
+            ent.ent_kv_append(self.ctx, B, k_new, v_new, block_tables, ctx_lens, k_cache, v_cache,
+                              ksum, stream)
+        else:
+            ent.ent_kv_append_q8(self.ctx, B, k_new, v_new, block_tables, ctx_lens, k_cache,
+                                 v_cache, k_scale, v_scale, ksum, stream)
+
+    def plan(self, B, n_new, ctx_lens, block_tables, free_ids, free_range, starts, slots,
+             new_lens=None, stream=None):
+        """Room for n_new more tokens per request; as many packed rows as slots has."""
+        ent.ent_prompt_plan(self.ctx, B, n_new, ctx_lens, block_tables, free_ids, free_ids.numel(),
+                            free_range, slots.numel(), starts, slots, new_lens, stream)
+
+    def store(self, k, v, slots, k_cache, v_cache, ksum, k_scale=None, v_scale=None, stream=None):
+        """Packed rows k, v [T, H_kv, d] (any row stride) into the cache at their slots."""
+        if k_scale is None:
+            ent.ent_prompt_store(self.ctx, k.shape[0], k, k.stride(0), v, v.stride(0), slots,
+                                 k_cache, v_cache, ksum, stream)
+        else:
+            ent.ent_prompt_store_q8(self.ctx, k.shape[0], k, k.stride(0), v, v.stride(0), slots,
+                                    k_cache, v_cache, k_scale, v_scale, ksum, stream)
+
+    def prompt(self, B, q, k, v, starts, out, lse=None, stream=None):
+        """Causal attention over packed rows q, out [T, H_q, d] and k, v [T, H_kv, d]."""
+        ent.ent_prompt_attention(self.ctx, B, q.shape[0], q, q.stride(0), k, k.stride(0), v,
+                                 v.stride(0), starts, out, out.stride(0), lse, stream)
 
     def device_status(self, stream=None) -> int:
         return ent.ent_device_status(self.ctx, stream)
