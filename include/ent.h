@@ -328,8 +328,10 @@ int ent_decode_step_append(ent_ctx* c, int B, const float* logits, long long ld,
  * Calls take at most ENT_MAX_PACKED_TOKENS rows (else ENT_E_UNSUPPORTED).
  * Row strides (ld*, in elements) let the queries, keys and values be parts of
  * one projection's rows; the H d values of a row are contiguous.  Strides are
- * whole multiples of 16 bytes, pointers 16-byte aligned. */
+ * whole multiples of 16 bytes and at most ENT_MAX_ROW_STRIDE elements, pointers
+ * 16-byte aligned. */
 #define ENT_MAX_PACKED_TOKENS (1 << 21)
+#define ENT_MAX_ROW_STRIDE (1 << 24)
 
 /* The place of a batch's new tokens: request b holds ctx_lens[b] tokens (0 for
  * a new prompt) and gets n_new[b] more (1 for every sequence makes room for a

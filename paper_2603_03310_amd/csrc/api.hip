@@ -108,7 +108,8 @@ int check_rows(ent_ctx* c, const char* who, int T) {
 }
 bool row_stride_ok(const ent_ctx* c, long long ld, int heads) {
   const int piece = c->cfg.kv_dtype == ENT_BF16 ? 8 : 4;
-  return ld >= static_cast<long long>(heads) * c->cfg.head_dim && ld % piece == 0;
+  return ld >= static_cast<long long>(heads) * c->cfg.head_dim && ld <= ENT_MAX_ROW_STRIDE &&
+         ld % piece == 0;
 }
 
 // An 8-bit cache needs a bf16 context with mean-key scoring.
@@ -127,7 +128,7 @@ int check_store(ent_ctx* c, const char* who, const void* k, long long ldk, const
   if (!k || !v || !slots || !k_cache || !v_cache || (!ksum && c->cfg.scoring != ENT_SCORE_EXACT))
     return fail(c, ENT_E_INVAL, std::string(who) + ": NULL required pointer");
   if (!row_stride_ok(c, ldk, c->cfg.num_kv_heads) || !row_stride_ok(c, ldv, c->cfg.num_kv_heads))
-    return fail(c, ENT_E_INVAL, std::string(who) + ": row strides need H_kv d elements or more, in 16-byte steps");
+    return fail(c, ENT_E_INVAL, std::string(who) + ": row strides need H_kv d to ENT_MAX_ROW_STRIDE elements, in 16-byte steps");
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
       !aligned(slots, 8))
     return fail(c, ENT_E_INVAL, std::string(who) + ": k, v and the caches need 16-byte alignment, slots 8");
@@ -557,7 +558,7 @@ int ent_prompt_attention(ent_ctx* c, int B, int T, const void* q, long long ldq,
   if (!row_stride_ok(c, ldq, Hq) || !row_stride_ok(c, ldo, Hq) || !row_stride_ok(c, ldk, Hkv) ||
       !row_stride_ok(c, ldv, Hkv))
     return fail(c, ENT_E_INVAL,
-                "ent_prompt_attention: row strides need the row's elements or more, in 16-byte steps");
+                "ent_prompt_attention: row strides need the row's elements to ENT_MAX_ROW_STRIDE, in 16-byte steps");
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16))
     return fail(c, ENT_E_INVAL, "ent_prompt_attention: q, k, v and out need 16-byte alignment");
   const hipError_t e = ent::launch_prompt_attention(c, B, T, q, ldq, k, ldk, v, ldv, starts, out, ldo,

@@ -31,7 +31,7 @@ EXPORTED = ("ent_default_config", "ent_check_config", "ent_row_stats_chunks", "e
             "ent_decode_step_append", "ent_prompt_plan", "ent_prompt_store",
             "ent_prompt_store_q8", "ent_prompt_attention", "ent_kv_append_q8",
             "ent_sparse_paged_decode_q8")
-ENT_MAX_PACKED_TOKENS = 1 << 21
+ENT_MAX_PACKED_TOKENS, ENT_MAX_ROW_STRIDE = 1 << 21, 1 << 24
 ENT_NOALLOC_SCRATCH_BYTES = 2 << 20
 ENT_SCHED_MAX_POOL = 8192
 

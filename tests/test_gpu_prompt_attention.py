@@ -96,6 +96,20 @@ def test_large_tiles_bf16(torch_cuda):
         _check(*r, "bf16")
 
 
+def test_every_split(torch_cuda):
+    """Row counts on either side of the rules that split the keys over waves, with lengths
+    that end in every part of a tile; batches of one to thousands of requests."""
+    rng = np.random.default_rng(8)
+    for heads, lens in [((4, 4, 128), [1024]), ((4, 4, 128), [1300, 77]), ((32, 8, 128), [250, 262, 1]),
+                        ((16, 4, 64), [2030]), ((16, 1, 64), [1100, 1070]),
+                        ((32, 8, 128), rng.integers(0, 12, 300).tolist()),
+                        ((8, 2, 64), rng.integers(0, 4, 3000).tolist()),
+                        ((64, 8, 64), rng.integers(1, 90, 70).tolist())]:
+        r = _run(torch_cuda, lens, heads, "bf16", seed=len(lens), max_batch=4096,
+                 max_blocks_per_seq=1)
+        _check(*r, "bf16")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [-0.11, 0.0, 0.9])
 def test_scales(torch_cuda, scale, dtype):
@@ -195,6 +209,7 @@ def test_refusals(torch_cuda):
                           (dict(out=None), ent.ENT_E_INVAL), (dict(ldq=248), ent.ENT_E_INVAL),
                           (dict(ldk=260), ent.ENT_E_INVAL), (dict(ldv=0), ent.ENT_E_INVAL),
                           (dict(ldo=255), ent.ENT_E_INVAL),
+                          (dict(ldk=ent.ENT_MAX_ROW_STRIDE + 8), ent.ENT_E_INVAL),
                           (dict(q=x.data_ptr() + 2), ent.ENT_E_INVAL),
                           (dict(out=out.data_ptr() + 8), ent.ENT_E_INVAL)]:
             with pytest.raises(ent.EntError) as e:
