@@ -407,7 +407,7 @@ int ent_prompt_attention(ent_ctx* c, int B, int T, const void* q, long long ldq,
  * saturate, NaN stay.  Scales that a caller makes must be finite and > 0. */
 
 /* ent_prompt_store into an 8-bit cache.  ksum: means of the keys as the cache
- * then holds them (scale * mean code). */
+ * then holds them (scale * mean code), 16-byte aligned. */
 int ent_prompt_store_q8(ent_ctx* c, int T, const void* k, long long ldk, const void* v,
                         long long ldv, const long long* slots, void* k_cache, void* v_cache,
                         float* k_scale, float* v_scale, float* ksum, void* stream);

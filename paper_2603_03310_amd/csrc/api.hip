@@ -8,6 +8,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <new>
 #include <string>
 
@@ -240,7 +241,7 @@ int ent_init(const ent_config* cfg, ent_ctx** out) {
   const size_t sz_ex = f.scoring == ENT_SCORE_EXACT
                            ? align_up(Bm * f.max_blocks_per_seq * f.num_q_heads * 2 * sizeof(float))
                            : 0;
-  const size_t sz_tick = align_up(Bm * sizeof(unsigned));
+  const size_t sz_tick = align_up(std::max(Bm, static_cast<size_t>(ent::kMinTickets)) * sizeof(unsigned));
   const size_t sz_flags = align_up(sizeof(unsigned));
   c->ws_bytes = sz_ent_part + sz_stats + sz_z + sz_lse + sz_lrow + sz_isc + sz_kphys + sz_acc + sz_ml +
                 sz_rec + sz_tmax + sz_ex + sz_tick + sz_flags;
@@ -537,6 +538,7 @@ int ent_prompt_store_q8(ent_ctx* c, int T, const void* k, long long ldk, const v
   if (int r = check_store(c, "ent_prompt_store_q8", k, ldk, v, ldv, slots, k_cache, v_cache, ksum))
     return r;
   if (!k_scale || !v_scale) return fail(c, ENT_E_INVAL, "ent_prompt_store_q8: NULL required pointer");
+  if (!aligned(ksum, 16)) return fail(c, ENT_E_INVAL, "ent_prompt_store_q8: ksum needs 16-byte alignment");
   const hipError_t e = ent::launch_prompt_store_q8(c, T, k, ldk, v, ldv, slots, k_cache, v_cache,
                                                    k_scale, v_scale, ksum,
                                                    static_cast<hipStream_t>(stream));
@@ -578,8 +580,9 @@ int ent_kv_append_q8(ent_ctx* c, int B, const void* k_new, const void* v_new,
   if (!k_new || !v_new || !block_tables || !ctx_lens || !k_cache || !v_cache || !k_scale || !v_scale ||
       !ksum)
     return fail(c, ENT_E_INVAL, "ent_kv_append_q8: NULL required pointer");
-  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16))
-    return fail(c, ENT_E_INVAL, "ent_kv_append_q8: k_new, v_new and the caches need 16-byte alignment");
+  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
+      !aligned(ksum, 16))
+    return fail(c, ENT_E_INVAL, "ent_kv_append_q8: k_new, v_new, the caches and ksum need 16-byte alignment");
   const hipError_t e = ent::launch_kv_append_q8(c, B, k_new, v_new, block_tables, ctx_lens, k_cache,
                                                 v_cache, k_scale, v_scale, ksum,
                                                 static_cast<hipStream_t>(stream));

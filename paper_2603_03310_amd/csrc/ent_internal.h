@@ -14,6 +14,7 @@ constexpr int kBlock = ENT_BLOCK_SIZE;      // tokens per KV block
 constexpr int kRowChunk = ENT_ROW_CHUNK;    // logits per entropy chunk
 constexpr int kMinScoreChunk = 16;          // smallest scoring chunk (blocks)
 constexpr int kMaxGroup = 16;               // query heads per KV head
+constexpr int kMinTickets = 1024;           // counters in the workspace, at least
 constexpr int kMaxBlocksPerSeq = 16384;     // selection keeps all scores in LDS
 constexpr int kEstChunkThreads = 256;       // threads of an entropy chunk job (maxima per chunk)
 constexpr float kLog2e = 1.4426950408889634f;
@@ -80,7 +81,8 @@ struct ent_ctx {
   int2* dec_rec = nullptr;        // [decode waves]  cut-segment records of the decode ranges
   float* tmax = nullptr;          // [max_batch, chunks, 256]  per-thread logit maxima (estimators)
   float2* exbuf = nullptr;        // [max_batch, MAXB, H_q]  exact mode: (log mass, mean logit) per block
-  unsigned* tickets = nullptr;    // [max_batch]  per-sequence counters of the fused step (zero between launches)
+  unsigned* tickets = nullptr;    // [max_batch, kMinTickets at least]  counters (zero between launches): per sequence in
+                                  // the fused step and the 8-bit append, of workgroups in the prompt plan
   unsigned* dev_flags = nullptr;  // [1]
 
   std::string err;

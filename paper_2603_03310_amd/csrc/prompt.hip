@@ -18,14 +18,20 @@ namespace {
 // first), so one launch does the whole plan: each workgroup then fills its part
 // of the slot map and of the new table entries, the first also writes starts
 // and lengths, and the one that finishes last moves the free list's head,
-// which all have read by then.
+// which all have read by then.  Who is last is counted in two steps, each counter
+// in a cache line of its own: counting costs about 10 ns a workgroup and line
+// (1.34M tokens of 256 requests: 14.4 us with 656 workgroups and one counter, 21.1
+// with 1312, 21.5 with their sixteen counters side by side, 9.0 so).
 //
 // Requests are admitted in order while tokens and blocks last; the inclusive
 // sums only grow, so "both fit" holds for a prefix of the batch and needs no
 // second pass.
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 256;
-constexpr int kPlanTokens = 2048;      // slots per workgroup
+constexpr int kPlanTokens = 1024;      // slots of a workgroup
+constexpr int kPlanCounters = 16;      // counters of finished workgroups, and one over them
+constexpr int kCounterPitch = 32;      // a cache line each
+static_assert((kPlanCounters + 1) * kCounterPitch <= kMinTickets, "counters");
 
 struct PlanArgs {
   const int* n_new;
@@ -38,7 +44,7 @@ struct PlanArgs {
   int* starts;
   long long* slots;
   int* new_lens;          // nullable
-  unsigned* ticket;       // 0 between launches
+  unsigned* tickets;      // kPlanCounters + 1 of them, 0 between launches
   unsigned* flags;
 };
 
@@ -68,9 +74,9 @@ __device__ __forceinline__ void plan_scan(int& a, int& b, int& ta, int& tb, int*
   b = ob;
 }
 
-// The largest b in [0, B) with s[b] <= x (s ascending, s[0] <= x).
-__device__ __forceinline__ int plan_find(const int* s, int B, int x) {
-  int lo = 0, hi = B;
+// The largest b in [from, to) with s[b] <= x (s ascending, s[from] <= x).
+__device__ __forceinline__ int plan_find(const int* s, int to, int x, int from) {
+  int lo = from, hi = to;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (s[mid] <= x) lo = mid; else hi = mid;
@@ -112,6 +118,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     if (b < a.B) {
       int n, ctx;
       request(b, n, ctx, bad);
+      s_tok[b] = n;
+      s_ctx[b] = ctx;
       tok += n;
       blk += (ctx + n + kBlock - 1) / kBlock - (ctx + kBlock - 1) / kBlock;
     }
@@ -124,13 +132,10 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   for (int i = 0; i < per; ++i) {
     const int b = t * per + i;
     if (b < a.B) {
-      int n, ctx;
-      unsigned f = 0;
-      request(b, n, ctx, f);
+      const int n = s_tok[b], ctx = s_ctx[b];          // its own of the loop before
       const int need = (ctx + n + kBlock - 1) / kBlock - (ctx + kBlock - 1) / kBlock;
       s_tok[b] = tok;
       s_blk[b] = blk;
-      s_ctx[b] = ctx;
       tok += n;
       blk += need;
       if (tok <= a.max_tokens && blk <= avail) {
@@ -165,39 +170,54 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   }
   __syncthreads();
 
-  // A free id by its place in the list, -1 (flagged) where it is no block.
-  auto free_id = [&](int i) {
-    const int p = a.ids[head + i];
-    if (p >= 0 && p < a.P) return p;
-    bad |= ENT_DEV_BAD_TABLE;
-    return -1;
-  };
-  // Slots of this workgroup's tokens, two consecutive ones a thread and step.
+  const bool pairs = (reinterpret_cast<uintptr_t>(a.slots) & 15) == 0;
+  // Slots of this workgroup's tokens, two consecutive ones a thread and step.  The
+  // requests that the tokens lie in are found within those of its first and last,
+  // mostly one or two; the block ids of all steps are then on their way together.
   const int t0 = blockIdx.x * kPlanTokens;
-  const int t1 = min(a.max_tokens, t0 + kPlanTokens);
-  auto slot_of = [&](int x) -> long long {
-    if (x >= total) return -1;
-    const int b = plan_find(s_tok, a.B, x);
-    const int pos = s_ctx[b] + x - s_tok[b];
-    const int j = pos / kBlock, have = (s_ctx[b] + kBlock - 1) / kBlock;
-    int p;
-    if (j < have) {
-      p = a.tables[static_cast<long long>(b) * a.MAXB + j];
-      if (p < 0 || p >= a.P) {
-        bad |= ENT_DEV_BAD_TABLE;
-        p = -1;
-      }
-    } else {
-      p = free_id(s_blk[b] + j - have);
+  const int t1 = min(total, t0 + kPlanTokens);           // tokens from here on are padding
+  constexpr int kPairs = kPlanTokens / (2 * kPlanThreads);
+  const int r0 = t0 < t1 ? plan_find(s_tok, a.B, t0, 0) : 0;
+  const int r1 = t0 < t1 ? plan_find(s_tok, a.B, t1 - 1, r0) + 1 : 0;
+  int page[2 * kPairs], row[2 * kPairs];
+#pragma unroll
+  for (int i = 0; i < 2 * kPairs; ++i) {
+    const int x = t0 + 2 * (t + i / 2 * kPlanThreads) + i % 2;
+    page[i] = row[i] = -1;
+    if (x < t1) {
+      const int b = plan_find(s_tok, r1, x, r0);
+      const int pos = s_ctx[b] + x - s_tok[b];
+      const int j = pos / kBlock, have = (s_ctx[b] + kBlock - 1) / kBlock;
+      row[i] = pos % kBlock;
+      page[i] = j < have ? a.tables[static_cast<long long>(b) * a.MAXB + j]
+                         : a.ids[head + s_blk[b] + j - have];
     }
-    return p < 0 ? -1 : static_cast<long long>(p) * kBlock + pos % kBlock;
-  };
-  for (int x = t0 + t; x < t1; x += kPlanThreads) a.slots[x] = slot_of(x);
+  }
+#pragma unroll
+  for (int i = 0; i < 2 * kPairs; i += 2) {
+    const int x = t0 + 2 * (t + i / 2 * kPlanThreads);
+    long long sl[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const bool ok = page[i + e] >= 0 && page[i + e] < a.P;
+      if (row[i + e] >= 0 && !ok) bad |= ENT_DEV_BAD_TABLE;
+      sl[e] = ok ? static_cast<long long>(page[i + e]) * kBlock + row[i + e] : -1;
+    }
+    if (x + 1 < a.max_tokens && pairs) {
+      *reinterpret_cast<longlong2*>(a.slots + x) = make_longlong2(sl[0], sl[1]);
+    } else {
+      if (x < a.max_tokens) a.slots[x] = sl[0];
+      if (x + 1 < a.max_tokens) a.slots[x + 1] = sl[1];
+    }
+  }
   // New table entries, dealt to all workgroups.
   for (int e = blockIdx.x * kPlanThreads + t; e < taken; e += gridDim.x * kPlanThreads) {
-    const int b = plan_find(s_blk, a.B, e);
+    const int b = plan_find(s_blk, a.B, e, 0);
     const int j = (s_ctx[b] + kBlock - 1) / kBlock + e - s_blk[b];
-    a.tables[static_cast<long long>(b) * a.MAXB + j] = free_id(e);
+    const int p = a.ids[head + e];
+    const bool ok = p >= 0 && p < a.P;
+    if (!ok) bad |= ENT_DEV_BAD_TABLE;
+    a.tables[static_cast<long long>(b) * a.MAXB + j] = ok ? p : -1;
   }
   if (blockIdx.x == 0) {
     for (int b = t; b <= a.B; b += kPlanThreads) {
@@ -207,8 +227,14 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   }
   if (bad) raise_flag(a.flags, bad);
   __syncthreads();
-  if (t == 0 && ring_ok && atomicInc(a.ticket, gridDim.x - 1) == gridDim.x - 1)
-    a.range[0] = head + taken;
+  if (t == 0 && ring_ok) {
+    const unsigned n = gridDim.x, c = blockIdx.x % kPlanCounters;
+    const unsigned mine = (n - c + kPlanCounters - 1) / kPlanCounters;        // workgroups of this counter
+    const unsigned used = n < kPlanCounters ? n : kPlanCounters;
+    if (atomicInc(a.tickets + c * kCounterPitch, mine - 1) == mine - 1 &&
+        atomicInc(a.tickets + kPlanCounters * kCounterPitch, used - 1) == used - 1)
+      a.range[0] = head + taken;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -361,25 +387,78 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreArgs a) {
 // old scale; codes; V transposed through LDS; old codes rounded again where the
 // scale grew; the mean of the keys that the cache then holds (a sum of 16 codes
 // is exact in 32 bits, so its order is free).  Thread (row, 8 dims).
+//
+// 16 elements a thread are few bytes for the work on them, so it is vector
+// instructions that bound it, before memory: magnitudes are compared as bf16 bits,
+// two at once, K's and V's maxima in one register; only a thread that holds
+// something not finite clamps; V is transposed by bytes of words.  51624 tokens of
+// 8 heads of 128: 94 us with float magnitudes, clamps throughout and single bytes,
+// 75 us so (331 MB, 87% of a large copy's rate).  Four tiles in turn a
+// workgroup with all loads issued at once: 113 against the 94.
 template <int D>
 struct Store8 {
   static constexpr int I = kBlock * D / 8;                            // threads of a tile
-  static constexpr int HW = kStoreThreads / I;
+  static constexpr int HW = kStoreThreads / I;                        // tiles of a workgroup
   static constexpr int WT = I / 64;                                   // waves of a tile
   static constexpr int PITCH = D + 16;
   __attribute__((aligned(16))) unsigned char k[HW * kBlock * PITCH];
   __attribute__((aligned(16))) unsigned char v[HW * kBlock * PITCH];
-  float top[2][kStoreThreads / 64];
+  unsigned top[kStoreThreads / 64];
 };
 
-__device__ __forceinline__ void load_bf16_row(const uint16_t* p, float (&x)[8]) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2_t pair16(unsigned x) { return __builtin_bit_cast(u16x2_t, x); }
+__device__ __forceinline__ unsigned pair32(u16x2_t x) { return __builtin_bit_cast(unsigned, x); }
+struct OpMaxPair {
+  __device__ __forceinline__ unsigned operator()(unsigned x, unsigned y) const {
+    return pair32(__builtin_elementwise_max(pair16(x), pair16(y)));
+  }
+};
+// Largest magnitude bits of eight bf16 values (0x7f80 and more: not finite).
+__device__ __forceinline__ unsigned top16(uint4 w) {
+  const unsigned m = 0x7fff7fffu;
+  OpMaxPair mx;
+  const u16x2_t x = pair16(mx(mx(w.x & m, w.y & m), mx(w.z & m, w.w & m)));
+  return max(static_cast<unsigned>(x.x), static_cast<unsigned>(x.y));
+}
+__device__ __forceinline__ void widen8(uint4 w, float (&x)[8]) {
   const unsigned u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = __uint_as_float(u[i] << 16);
     x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
   }
+}
+// ... of those that are finite.
+__device__ __forceinline__ unsigned top16_finite(uint4 w) {
+  float x[8], t = 0.f;
+  widen8(w, x);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t = fmaxf(t, q8_mag(x[i]));
+  return __float_as_uint(t) >> 16;
+}
+// Eight codes of x / s (inv = 1 / s: exact but for a kept scale of the caller's own
+// making that is no power of two).  Finite values stay under 464, which rounds to
+// 448, as the scale covers them.
+__device__ __forceinline__ uint2 codes8(uint4 w, float inv, bool clamp) {
+  float y[8];
+  widen8(w, y);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] *= inv;
+  if (clamp) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = q8_clamp(y[i]);
+  }
+  return make_uint2(q8_pack4(y[0], y[1], y[2], y[3]), q8_pack4(y[4], y[5], y[6], y[7]));
+}
+// Eight codes times f <= 1, rounded again.
+__device__ __forceinline__ uint2 recode8(uint2 w, float f) {
+  float y[8];
+  q8_unpack4(w.x, y);
+  q8_unpack4(w.y, y + 4);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] *= f;
+  return make_uint2(q8_pack4(y[0], y[1], y[2], y[3]), q8_pack4(y[4], y[5], y[6], y[7]));
 }
 
 template <int D>
@@ -393,70 +472,42 @@ __device__ __forceinline__ void store8_run(const StoreArgs& a, Store8<D>& sh, in
   const long long tg = static_cast<long long>(p) * a.Hkv + g;
   unsigned char* kc = static_cast<unsigned char*>(a.kc) + tg * kBlock * D;
   unsigned char* vc = static_cast<unsigned char*>(a.vc) + tg * kBlock * D;
-  float kx[8], vx[8];
-  uint2 kold = make_uint2(0u, 0u), vold = kold;
+  uint4 kx = make_uint4(0u, 0u, 0u, 0u), vx = kx;
+  uint2 kold = make_uint2(0u, 0u);
   float ks0 = 0.f, vs0 = 0.f;
   if (fresh) {
-    load_bf16_row(k + (row - row0) * a.ldk + g * D + c, kx);
-    load_bf16_row(v + (row - row0) * a.ldv + g * D + c, vx);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) kx[i] = vx[i] = 0.f;
+    kx = *reinterpret_cast<const uint4*>(k + (row - row0) * a.ldk + g * D + c);
+    vx = *reinterpret_cast<const uint4*>(v + (row - row0) * a.ldv + g * D + c);
   }
   if (head && row0 > 0) {
     ks0 = a.ks[tg];
     vs0 = a.vs[tg];
     if (old) kold = *reinterpret_cast<const uint2*>(kc + row * D + c);
   }
-  float kt = 0.f, vt = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    kt = fmaxf(kt, q8_mag(kx[i]));
-    vt = fmaxf(vt, q8_mag(vx[i]));
-  }
-  kt = wave_max(kt);
-  vt = wave_max(vt);
+  unsigned kt = top16(kx), vt = top16(vx);
+  const bool kbad = kt >= 0x7f80u, vbad = vt >= 0x7f80u;
+  if (kbad) kt = top16_finite(kx);
+  if (vbad) vt = top16_finite(vx);
+  const unsigned both = wave_reduce(kt << 16 | vt, OpMaxPair());
   __syncthreads();                    // the last run's LDS is read no more
-  if ((t & 63) == 0) {
-    sh.top[0][t >> 6] = kt;
-    sh.top[1][t >> 6] = vt;
-  }
+  if ((t & 63) == 0) sh.top[t >> 6] = both;
   __syncthreads();
-  kt = vt = 0.f;
+  unsigned top = 0;
 #pragma unroll
-  for (int w = 0; w < S::WT; ++w) {
-    kt = fmaxf(kt, sh.top[0][hh * S::WT + w]);
-    vt = fmaxf(vt, sh.top[1][hh * S::WT + w]);
-  }
-  const float kn = q8_scale(kt), vn = q8_scale(vt);
+  for (int w = 0; w < S::WT; ++w) top = OpMaxPair()(top, sh.top[hh * S::WT + w]);
+  const float kn = q8_scale(__uint_as_float(top & 0xffff0000u)), vn = q8_scale(__uint_as_float(top << 16));
   const float ks = row0 > 0 && ks0 > kn ? ks0 : kn, vs = row0 > 0 && vs0 > vn ? vs0 : vn;
   const bool kgrow = row0 > 0 && ks > ks0, vgrow = row0 > 0 && vs > vs0;
-  // The reciprocal is exact but for a kept scale of the caller's own making
-  // that is no power of two.
-  auto codes = [](const float (&x)[8], float s) {
-    const float inv = __fdiv_rn(1.f, s);
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = x[i] * inv;
-    return make_uint2(q8_pack4(y[0], y[1], y[2], y[3]), q8_pack4(y[4], y[5], y[6], y[7]));
-  };
-  auto again = [](uint2 w, float f) {
-    float y[8];
-    q8_unpack4(w.x, y);
-    q8_unpack4(w.y, y + 4);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] *= f;
-    return make_uint2(q8_pack4(y[0], y[1], y[2], y[3]), q8_pack4(y[4], y[5], y[6], y[7]));
-  };
   unsigned char* const lk = sh.k + (hh * kBlock + row) * S::PITCH + c;
   if (fresh) {
-    const uint2 kw = codes(kx, ks);
+    const uint2 kw = codes8(kx, __fdiv_rn(1.f, ks), kbad);
     *reinterpret_cast<uint2*>(kc + row * D + c) = kw;
     *reinterpret_cast<uint2*>(lk) = kw;
-    *reinterpret_cast<uint2*>(sh.v + (hh * kBlock + row) * S::PITCH + c) = codes(vx, vs);
+    *reinterpret_cast<uint2*>(sh.v + (hh * kBlock + row) * S::PITCH + c) =
+        codes8(vx, __fdiv_rn(1.f, vs), vbad);
   } else if (old) {
     if (kgrow) {
-      kold = again(kold, ks0 / ks);
+      kold = recode8(kold, ks0 / ks);
       *reinterpret_cast<uint2*>(kc + row * D + c) = kold;
     }
     *reinterpret_cast<uint2*>(lk) = kold;
@@ -466,21 +517,45 @@ __device__ __forceinline__ void store8_run(const StoreArgs& a, Store8<D>& sh, in
     a.vs[tg] = vs;
   }
   __syncthreads();
-  // V: a thread has 8 rows of one dim.
-  const int d = r / 2, s0 = r % 2 * 8;
-  if (head && s0 < row1) {
-    unsigned char* const at = vc + d * kBlock + s0;
-    if (vgrow && s0 < row0) vold = again(*reinterpret_cast<const uint2*>(at), vs0 / vs);
-    unsigned char x[8];
-    __builtin_memcpy(x, &vold, 8);
+  if (rows == kBlock) {
+    // A whole block's V: a thread turns 8 rows of 4 dims.
+    for (int e = r; e < D / 2; e += S::I) {
+      const int d = e / 2 * 4, s0 = e % 2 * 8;
+      unsigned w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (s0 + i >= row0 && s0 + i < row1) x[i] = sh.v[(hh * kBlock + s0 + i) * S::PITCH + d];
-    if (s0 >= row0 && s0 + 8 <= row1) {
-      uint2 w;
-      __builtin_memcpy(&w, x, 8);
-      *reinterpret_cast<uint2*>(at) = w;
-    } else {
+      for (int i = 0; i < 8; ++i)
+        w[i] = *reinterpret_cast<const unsigned*>(sh.v + (hh * kBlock + s0 + i) * S::PITCH + d);
+      uint2 o[4];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        // Bytes 0 and 1, then 2 and 3, of pairs of rows; then dims.
+        const unsigned a0 = __builtin_amdgcn_perm(w[4 * z + 1], w[4 * z], 0x05010400u);
+        const unsigned a1 = __builtin_amdgcn_perm(w[4 * z + 1], w[4 * z], 0x07030602u);
+        const unsigned b0 = __builtin_amdgcn_perm(w[4 * z + 3], w[4 * z + 2], 0x05010400u);
+        const unsigned b1 = __builtin_amdgcn_perm(w[4 * z + 3], w[4 * z + 2], 0x07030602u);
+        const unsigned q[4] = {__builtin_amdgcn_perm(b0, a0, 0x05040100u), __builtin_amdgcn_perm(b0, a0, 0x07060302u),
+                               __builtin_amdgcn_perm(b1, a1, 0x05040100u), __builtin_amdgcn_perm(b1, a1, 0x07060302u)};
+#pragma unroll
+        for (int y = 0; y < 4; ++y) (z ? o[y].y : o[y].x) = q[y];
+      }
+      if (head) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) *reinterpret_cast<uint2*>(vc + (d + y) * kBlock + s0) = o[y];
+      }
+    }
+  } else if (head) {
+    // Part of one: a thread has 8 rows of one dim; the others stay as they are,
+    // but for earlier ones that a larger scale rounds again.
+    const int d = r / 2, s0 = r % 2 * 8;
+    if (s0 < row1) {
+      unsigned char* const at = vc + d * kBlock + s0;
+      uint2 vold = make_uint2(0u, 0u);
+      if (vgrow && s0 < row0) vold = recode8(*reinterpret_cast<const uint2*>(at), vs0 / vs);
+      unsigned char x[8];
+      __builtin_memcpy(x, &vold, 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (s0 + i >= row0 && s0 + i < row1) x[i] = sh.v[(hh * kBlock + s0 + i) * S::PITCH + d];
       const int first = vgrow ? 0 : row0;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -488,14 +563,22 @@ __device__ __forceinline__ void store8_run(const StoreArgs& a, Store8<D>& sh, in
     }
   }
   if (a.ksum && head) {
-    for (int e = r; e < D; e += S::I) {
-      float sum = 0.f;
+    // Four dims a thread, from the tile's last threads on (the first turn V).
+    for (int e = S::I - 1 - r; e < D / 4; e += S::I) {
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < kBlock; ++s) {
-        const q8_f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(sh.k[(hh * kBlock + s) * S::PITCH + e], false);
-        if (s < row1) sum += x.x;
+        float x[4];
+        q8_unpack4(*reinterpret_cast<const unsigned*>(sh.k + (hh * kBlock + s) * S::PITCH + 4 * e), x);
+        if (s < row1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] += x[i];
+        }
       }
-      a.ksum[tg * D + e] = __fdiv_rn(sum, static_cast<float>(row1)) * ks;
+      const float n = static_cast<float>(row1);
+      *reinterpret_cast<float4*>(a.ksum + tg * D + 4 * e) =
+          make_float4(__fdiv_rn(sum[0], n) * ks, __fdiv_rn(sum[1], n) * ks, __fdiv_rn(sum[2], n) * ks,
+                      __fdiv_rn(sum[3], n) * ks);
     }
   }
 }
@@ -601,9 +684,9 @@ hipError_t launch_prompt_store_q8(const ent_ctx* c, int T, const void* k, long l
   a.vs = v_scale;
   const int n = (T + kBlock - 1) / kBlock;
   if (c->cfg.head_dim == 128)
-    hipLaunchKernelGGL(store_q8_kernel<128>, store_grid<Store8<128>::HW>(c, n), dim3(kStoreThreads), 0, s, a);
+    hipLaunchKernelGGL(store_q8_kernel<128>, (store_grid<Store8<128>::HW>(c, n)), dim3(kStoreThreads), 0, s, a);
   else
-    hipLaunchKernelGGL(store_q8_kernel<64>, store_grid<Store8<64>::HW>(c, n), dim3(kStoreThreads), 0, s, a);
+    hipLaunchKernelGGL(store_q8_kernel<64>, (store_grid<Store8<64>::HW>(c, n)), dim3(kStoreThreads), 0, s, a);
   return hipGetLastError();
 }
 
@@ -616,10 +699,10 @@ hipError_t launch_kv_append_q8(const ent_ctx* c, int B, const void* k_new, const
   a.vs = v_scale;
   const int MAXB = c->cfg.max_blocks_per_seq;
   if (c->cfg.head_dim == 128)
-    hipLaunchKernelGGL(append_q8_kernel<128>, store_grid<Store8<128>::HW>(c, B), dim3(kStoreThreads), 0,
+    hipLaunchKernelGGL(append_q8_kernel<128>, (store_grid<Store8<128>::HW>(c, B)), dim3(kStoreThreads), 0,
                        s, a, tables, ctx_lens, MAXB, c->tickets);
   else
-    hipLaunchKernelGGL(append_q8_kernel<64>, store_grid<Store8<64>::HW>(c, B), dim3(kStoreThreads), 0,
+    hipLaunchKernelGGL(append_q8_kernel<64>, (store_grid<Store8<64>::HW>(c, B)), dim3(kStoreThreads), 0,
                        s, a, tables, ctx_lens, MAXB, c->tickets);
   return hipGetLastError();
 }

@@ -34,15 +34,16 @@ __device__ __forceinline__ float q8_scale(float top) {
   k = max(k, kQ8MinExp);
   return __uint_as_float(static_cast<unsigned>(k + 127) << 23);
 }
-// Four codes of a .. d, the first in the low byte: rounded to nearest
-// even, clamped to +-448 (which a NaN passes).
+// x clamped to +-448; a NaN passes.
 __device__ __forceinline__ float q8_clamp(float x) {
   x = x > kQ8Top ? kQ8Top : x;
   return x < -kQ8Top ? -kQ8Top : x;
 }
+// Four codes, the first in the low byte, rounded to nearest even (464 and more, and
+// infinities, become NaN: clamp first where they can occur).
 __device__ __forceinline__ unsigned q8_pack4(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(q8_clamp(a), q8_clamp(b), 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(q8_clamp(c), q8_clamp(d), w, true);
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
   return static_cast<unsigned>(w);
 }
 __device__ __forceinline__ void q8_unpack4(unsigned w, float* x) {

@@ -329,11 +329,13 @@ def test_refusals(torch_cuda):
         good8 = dict(good, k_scale=sc, v_scale=sc)
         refuse(lambda **k: ent.ent_prompt_store(dec.ctx, **k), good, common)
         refuse(lambda **k: ent.ent_prompt_store_q8(dec.ctx, **k), good8,
-               common + [(dict(k_scale=None), I), (dict(v_scale=None), I)])
+               common + [(dict(k_scale=None), I), (dict(v_scale=None), I),
+                         (dict(ksum=ksum.data_ptr() + 4), I)])
         app = dict(B=2, k_new=x, v_new=x, block_tables=tab, ctx_lens=ctx, k_cache=kc, v_cache=kc,
                    k_scale=sc, v_scale=sc, ksum=ksum)
         refuse(lambda **k: ent.ent_kv_append_q8(dec.ctx, **k), app,
-               [(dict(B=3), I), (dict(B=-1), I), (dict(k_new=x.data_ptr() + 2), I)] +
+               [(dict(B=3), I), (dict(B=-1), I), (dict(k_new=x.data_ptr() + 2), I),
+                (dict(ksum=ksum.data_ptr() + 8), I)] +
                [({f: None}, I) for f in app if f != "B"])
         dcd = dict(B=2, q=x, k_cache=kc, v_cache=kc, k_scale=sc, v_scale=sc, block_tables=tab,
                    ctx_lens=ctx, kept=tab, n_kept=ctx, out=ksum)
