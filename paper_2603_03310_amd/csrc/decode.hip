@@ -736,13 +736,13 @@ __global__ __launch_bounds__(kThreads, 2) void decode_q8_kernel(DecodeArgs a) {
     const int pk = max(__shfl(win.p, i + min(r16 >> 2, n - 1)), 0);
     const int pv = max(__shfl(win.p, i + min(gq, n - 1)), 0);
     const unsigned char* kt = kc + (static_cast<long long>(pk) * a.Hkv + g) * kBlock * D +
-                              (r16 & 3) * D + gq * (D / 4);
+                              (r16 & 3) * D + 16 * gq;
     const unsigned char* vt = vc + (static_cast<long long>(pv) * a.Hkv + g) * kBlock * D + r16 * kBlock;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int y = 0; y < KL; ++y)
-        x[t * KL + y] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kt + 4 * t * D + 16 * y));
+        x[t * KL + y] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kt + 4 * t * D + 64 * y));
 #pragma unroll
     for (int m = 0; m < MT; ++m)
       x[4 * KL + m] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vt + 16 * m * kBlock));
@@ -766,10 +766,11 @@ __global__ __launch_bounds__(kThreads, 2) void decode_q8_kernel(DecodeArgs a) {
     cur_seg = seg;
     const int b = seg / a.Hkv, g = seg % a.Hkv;
     const long long qh = static_cast<long long>(b) * Hq + g * a.G + r16;
-    // Step ks of lane (., gq) is dims gq D / 4 + 8 ks .. + 7, as in its K pieces.
+    // Step ks of lane (., gq) is eight dims of its K piece ks / 2: 64 (ks / 2) + 16 gq
+    // + 8 (ks % 2) on.
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      if (head_ok) qreg[ks] = load_bf16x8(q + qh * D + gq * (D / 4) + 8 * ks);
+      if (head_ok) qreg[ks] = load_bf16x8(q + qh * D + 64 * (ks / 2) + 16 * gq + 8 * (ks % 2));
       else qreg[ks] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
     }
     m_run = -INFINITY;
