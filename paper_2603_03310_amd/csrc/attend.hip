@@ -532,7 +532,10 @@ template <int D, int RG, int KG>
 struct AttF32 {
   static constexpr int BT = 32 * KG;
   static constexpr int PK = D + 4, PV = D + 8;              // V's rows four apart: 32 banks apart
-  static constexpr int NBUF = 2 * BT * (PK + PV) * 4 <= 150000 ? 2 : 1;
+  // Two buffers where two workgroups still fit a CU's LDS; else one, and a barrier more a
+  // tile.  us at one workgroup of two buffers and two of one (8 / 8 heads of 64): four
+  // requests of 2000 tokens 288, 219; of 176 to 464 tokens 22.7, 23.6.
+  static constexpr int NBUF = 2 * BT * (PK + PV) * 4 <= 76000 ? 2 : 1;
   union {
     struct {
       __attribute__((aligned(16))) float k[NBUF][BT * PK];
@@ -732,20 +735,27 @@ hipError_t launch_prompt_attention(const ent_ctx* c, int B, int T, const void* q
   a.flip = c->cfg.scale < 0.f ? 0x80008000u : 0u;
   a.keep = c->cfg.scale == 0.f ? 0u : 0xffffffffu;
   if (a.c == 0.f) a.c = 1.f;
-  // Split the keys over waves where the rows alone do not fill the CUs: where half
-  // or a quarter of the rows a workgroup still gives each CU one at most or where few long requests leave CUs idle behind the longest
-  // rows.  us with 256, 128 and 64 rows a workgroup: one request of 512 tokens (32 / 8
-  // heads of 128) 18.1, 13.5, 12.5; four of 300 15.3, 20.1, 30.0; one of 2500 65.8, 69.0,
-  // 91.9; 3000 and 500 tokens (16 / 1 heads of 64) 55.0, 35.7, 38.4.
+  // The keys are split over waves where the rows alone do not fill the CUs: a workgroup
+  // takes a half or a quarter of the rows while that leaves each CU one at most, and a
+  // half also where requests of 1024 tokens and more would leave CUs idle behind the
+  // longest rows.  us with 256, 128 and 64 rows a workgroup: one request of 512 tokens
+  // (32 / 8 heads of 128) 18.1, 13.5, 12.5; four of 300 15.3, 20.1, 30.0; one of 2500
+  // 65.8, 69.0, 91.9; 3000 and 500 tokens (16 / 1 heads of 64) 55.0, 35.7, 38.4.
   const long long rows = static_cast<long long>(T) * a.G * a.Hkv;
   const long long cus = c->num_cu;
   if (!bf16) {
-    const bool wide = rows >= 256 * cus;
+    // Fewer rows a workgroup here, since each takes longer.  us with 128, 64 and 32 rows a
+    // workgroup: eight requests of 2048 tokens (32 / 8 heads of 128) 2720, 3090, -; one of
+    // 1000 163, 106, 140; four of 2000 (8 / 8 heads of 64) 240, 201, 219; one of 2000 -,
+    // 107, 76; 300, 500 and 700 (16 / 4) 69, 46, 39.
+    const int rg = rows >= 256 * cus ? 4 : rows >= 96 * cus ? 2 : 1;
     if (c->cfg.head_dim == 128)
-      return wide ? att_launch(attend_f32_kernel<128, 4, 1>, 128, kAttF32Threads, a, s)
-                  : att_launch(attend_f32_kernel<128, 1, 4>, 32, kAttF32Threads, a, s);
-    return wide ? att_launch(attend_f32_kernel<64, 4, 1>, 128, kAttF32Threads, a, s)
-                : att_launch(attend_f32_kernel<64, 1, 4>, 32, kAttF32Threads, a, s);
+      return rg == 4   ? att_launch(attend_f32_kernel<128, 4, 1>, 128, kAttF32Threads, a, s)
+             : rg == 2 ? att_launch(attend_f32_kernel<128, 2, 2>, 64, kAttF32Threads, a, s)
+                       : att_launch(attend_f32_kernel<128, 1, 4>, 32, kAttF32Threads, a, s);
+    return rg == 4   ? att_launch(attend_f32_kernel<64, 4, 1>, 128, kAttF32Threads, a, s)
+           : rg == 2 ? att_launch(attend_f32_kernel<64, 2, 2>, 64, kAttF32Threads, a, s)
+                     : att_launch(attend_f32_kernel<64, 1, 4>, 32, kAttF32Threads, a, s);
   }
   const int split = rows <= 64 * cus ? 4
                     : rows <= 128 * cus || (rows < 256 * cus && T >= 1024ll * B) ? 2 : 1;

@@ -110,6 +110,15 @@ def test_every_split(torch_cuda):
         _check(*r, "bf16")
 
 
+def test_every_split_fp32(torch_cuda):
+    """The same on either side of the fp32 rules: 24576 and 65536 rows at 256 compute units."""
+    for heads, lens in [((8, 8, 64), [1500, 1570]), ((8, 8, 64), [1500, 1571, 2]), ((32, 8, 128), [767]),
+                        ((32, 8, 128), [700, 69]), ((16, 1, 64), [2049, 2046]), ((16, 1, 128), [1, 2050, 2046]),
+                        ((64, 32, 64), [1, 700, 333])]:
+        r = _run(torch_cuda, lens, heads, "f32", seed=len(lens), max_blocks_per_seq=1)
+        _check(*r, "f32")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [-0.11, 0.0, 0.9])
 def test_scales(torch_cuda, scale, dtype):
