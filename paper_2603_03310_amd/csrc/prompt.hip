@@ -160,6 +160,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     taken = max(taken, s_red[kPlanThreads / 64 + w]);
   }
   if (all_tok > total || all_blk > taken) bad |= ENT_DEV_CACHE_FULL;
+  // Every workgroup finds the same here; the first raises it (an atomic of each, where
+  // the free list ran out: 65.9 us instead of 6.8 with 656 workgroups).
+  if (blockIdx.x != 0) bad = 0;
   for (int b = t; b < a.B; b += kPlanThreads) {
     s_tok[b] = min(s_tok[b], total);
     s_blk[b] = min(s_blk[b], taken);
