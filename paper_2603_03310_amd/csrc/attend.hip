@@ -99,6 +99,7 @@ __device__ __forceinline__ bool att_stretch(const AttArgs& a, int i, int lg_ntok
   // The request: of those with more than lo stretches, number i - above.
   int want = i - above, b0 = 0;
   for (;; b0 += 64) {
+    if (b0 >= a.B) return false;            // starts so far from ascending that the sums passed 32 bits
     const unsigned long long has = __ballot(count(b0 + lane) > lo);
     const int n = __popcll(has);
     if (want < n) {
