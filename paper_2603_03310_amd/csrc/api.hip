@@ -502,8 +502,8 @@ int ent_prompt_plan(ent_ctx* c, int B, const int* n_new, const int* ctx_lens, in
   if (!n_new || !ctx_lens || !block_tables || (!free_ids && n_ids > 0) || !free_range || !starts ||
       (!slots && max_tokens > 0))
     return fail(c, ENT_E_INVAL, "ent_prompt_plan: NULL required pointer");
-  if (new_lens && (new_lens == n_new || new_lens == ctx_lens))
-    return fail(c, ENT_E_INVAL, "ent_prompt_plan: new_lens aliases n_new or ctx_lens");
+  if ((new_lens && (new_lens == n_new || new_lens == ctx_lens)) || starts == n_new || starts == ctx_lens)
+    return fail(c, ENT_E_INVAL, "ent_prompt_plan: new_lens or starts aliases n_new or ctx_lens");
   if (!aligned(slots, 8)) return fail(c, ENT_E_INVAL, "ent_prompt_plan: slots needs 8-byte alignment");
   const hipError_t e = ent::launch_prompt_plan(c, B, n_new, ctx_lens, block_tables, free_ids, n_ids,
                                                free_range, max_tokens, starts, slots, new_lens,
@@ -563,6 +563,8 @@ int ent_prompt_attention(ent_ctx* c, int B, int T, const void* q, long long ldq,
                 "ent_prompt_attention: row strides need the row's elements to ENT_MAX_ROW_STRIDE, in 16-byte steps");
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16))
     return fail(c, ENT_E_INVAL, "ent_prompt_attention: q, k, v and out need 16-byte alignment");
+  if (out == q || out == k || out == v)
+    return fail(c, ENT_E_INVAL, "ent_prompt_attention: out aliases q, k or v");
   const hipError_t e = ent::launch_prompt_attention(c, B, T, q, ldq, k, ldk, v, ldv, starts, out, ldo,
                                                     lse, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(c, e, "ent_prompt_attention launch");

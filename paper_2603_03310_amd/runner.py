@@ -82,17 +82,29 @@ class Decoder:
 
     def store(self, k, v, slots, k_cache, v_cache, ksum, k_scale=None, v_scale=None, stream=None):
         """Packed rows k, v [T, H_kv, d] (any row stride) into the cache at their slots."""
+        T = k.shape[0]
+        ldk, ldv = (self._rows(x, T, self.cfg.num_kv_heads) for x in (k, v))
+        if slots.numel() != T:
+            raise ent.EntError(ent.ENT_E_INVAL, f"{slots.numel()} slots for {T} rows")
         if k_scale is None:
-            ent.ent_prompt_store(self.ctx, k.shape[0], k, k.stride(0), v, v.stride(0), slots,
-                                 k_cache, v_cache, ksum, stream)
+            ent.ent_prompt_store(self.ctx, T, k, ldk, v, ldv, slots, k_cache, v_cache, ksum, stream)
         else:
-            ent.ent_prompt_store_q8(self.ctx, k.shape[0], k, k.stride(0), v, v.stride(0), slots,
-                                    k_cache, v_cache, k_scale, v_scale, ksum, stream)
+            ent.ent_prompt_store_q8(self.ctx, T, k, ldk, v, ldv, slots, k_cache, v_cache, k_scale,
+                                    v_scale, ksum, stream)
 
     def prompt(self, B, q, k, v, starts, out, lse=None, stream=None):
         """Causal attention over packed rows q, out [T, H_q, d] and k, v [T, H_kv, d]."""
-        ent.ent_prompt_attention(self.ctx, B, q.shape[0], q, q.stride(0), k, k.stride(0), v,
-                                 v.stride(0), starts, out, out.stride(0), lse, stream)
+        T, Hq, Hkv = q.shape[0], self.cfg.num_q_heads, self.cfg.num_kv_heads
+        ldq, ldk, ldv, ldo = (self._rows(x, T, H) for x, H in ((q, Hq), (k, Hkv), (v, Hkv), (out, Hq)))
+        ent.ent_prompt_attention(self.ctx, B, T, q, ldq, k, ldk, v, ldv, starts, out, ldo, lse, stream)
+
+    def _rows(self, x, T, heads):
+        """The row stride of T packed rows of whole heads, side by side."""
+        d = self.cfg.head_dim
+        if x.shape != (T, heads, d) or x.stride(2) != 1 or (heads > 1 and x.stride(1) != d):
+            raise ent.EntError(ent.ENT_E_INVAL, f"rows of shape {tuple(x.shape)} and strides "
+                                                f"{x.stride()}: [{T}, {heads}, {d}] needed, each row in one piece")
+        return x.stride(0)
 
     def device_status(self, stream=None) -> int:
         return ent.ent_device_status(self.ctx, stream)

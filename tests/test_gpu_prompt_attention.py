@@ -220,7 +220,8 @@ def test_refusals(torch_cuda):
                           (dict(ldo=255), ent.ENT_E_INVAL),
                           (dict(ldk=ent.ENT_MAX_ROW_STRIDE + 8), ent.ENT_E_INVAL),
                           (dict(q=x.data_ptr() + 2), ent.ENT_E_INVAL),
-                          (dict(out=out.data_ptr() + 8), ent.ENT_E_INVAL)]:
+                          (dict(out=out.data_ptr() + 8), ent.ENT_E_INVAL),
+                          (dict(out=x), ent.ENT_E_INVAL)]:
             with pytest.raises(ent.EntError) as e:
                 ent.ent_prompt_attention(dec.ctx, **{**good, **bad})
             assert e.value.code == code, bad
@@ -236,3 +237,60 @@ def test_another_stream_and_no_lse(torch_cuda):
     with torch.cuda.stream(s):
         r = _run(torch, [300, 20], (8, 2, 128), "bf16", lse=False)
     _check(*r, "bf16")
+
+
+def test_largest_batch(torch_cuda):
+    """4096 requests of none to three tokens, in every split of either type."""
+    lens = np.random.default_rng(9).integers(0, 4, 4096).tolist()
+    for heads, dtype in [((2, 2, 128), "bf16"), ((4, 2, 128), "bf16"), ((16, 2, 128), "bf16"),
+                         ((2, 2, 128), "f32"), ((6, 6, 64), "f32"), ((16, 1, 128), "f32")]:
+        r = _run(torch_cuda, lens, heads, dtype, seed=9, max_batch=4096, max_blocks_per_seq=1)
+        _check(*r, dtype)
+
+
+def test_two_streams_at_once(torch_cuda):
+    """One handle, two calls in flight: the operator keeps nothing in the handle."""
+    torch = torch_cuda
+    from paper_2603_03310_amd.runner import Decoder
+    lens = [[1700, 3], [40, 900, 1]]
+    xs = [torch.randn(sum(n), 16, 128, device="cuda:0").to(torch.bfloat16) for n in lens]
+    st = [torch.tensor(np.concatenate([[0], np.cumsum(n)]), dtype=torch.int32, device="cuda:0") for n in lens]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    with Decoder(**config(8, 4, 128)) as dec:
+        def go(i, out, stream):
+            x = xs[i]
+            dec.prompt(len(lens[i]), x[:, :8], x[:, 8:12], x[:, 12:], st[i], out, stream=stream)
+        want = [torch.zeros(len(x), 8, 128, dtype=x.dtype, device="cuda:0") for x in xs]
+        got = [[torch.zeros_like(w) for w in want] for _ in range(4)]
+        for i in (0, 1):
+            go(i, want[i], None)
+        torch.cuda.synchronize()
+        for pair in got:
+            for i in (0, 1):
+                go(i, pair[i], streams[i].cuda_stream)
+        torch.cuda.synchronize()
+        for pair in got:
+            assert all(torch.equal(a, b) for a, b in zip(pair, want))
+
+
+def test_the_wrapper_refuses_rows_in_pieces(torch_cuda):
+    torch = torch_cuda
+    from paper_2603_03310_amd import ent
+    from paper_2603_03310_amd.runner import Decoder
+    x = torch.zeros(8, 4, 64, dtype=torch.bfloat16, device="cuda:0")
+    st = torch.tensor([0, 8], dtype=torch.int32, device="cuda:0")
+    heads_first = torch.zeros(4, 8, 64, dtype=torch.bfloat16, device="cuda:0").transpose(0, 1)
+    with Decoder(**config(4, 4, 64, num_pool_blocks=4)) as dec:
+        good = dict(q=x, k=x.clone(), v=x.clone(), out=torch.zeros_like(x))
+        kc, ksum = torch.zeros(4, 4, 16, 64, dtype=x.dtype, device="cuda:0"), torch.zeros(4, 4, 64, device="cuda:0")
+        for name in good:
+            for bad in (heads_first, x[:7].clone(), x[:, :2].clone(), torch.zeros_like(x).mT):
+                with pytest.raises(ent.EntError) as e:
+                    dec.prompt(1, **{**good, name: bad}, starts=st)
+                assert e.value.code == ent.ENT_E_INVAL
+        slots = torch.arange(8, device="cuda:0")
+        for kw in (dict(k=heads_first), dict(v=x[:7]), dict(slots=slots[:7])):
+            with pytest.raises(ent.EntError):
+                dec.store(**{**dict(k=x, v=x, slots=slots, k_cache=kc, v_cache=kc, ksum=ksum), **kw})
+        dec.prompt(1, **good, starts=st)
+        torch.cuda.synchronize()

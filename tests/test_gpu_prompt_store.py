@@ -318,7 +318,7 @@ def test_refusals(torch_cuda):
                 (dict(max_tokens=ent.ENT_MAX_PACKED_TOKENS + 1), U), (dict(n_new=None), I),
                 (dict(ctx_lens=None), I), (dict(block_tables=None), I), (dict(free_ids=None), I),
                 (dict(free_range=None), I), (dict(starts=None), I), (dict(slots=None), I),
-                (dict(new_lens=ctx), I), (dict(new_lens=n_new), I),
+                (dict(new_lens=ctx), I), (dict(new_lens=n_new), I), (dict(starts=ctx), I), (dict(starts=n_new), I),
                 (dict(slots=slots.data_ptr() + 4), I)])
         common = [(dict(T=-1), I), (dict(T=ent.ENT_MAX_PACKED_TOKENS + 1), U), (dict(k=None), I),
                   (dict(v=None), I), (dict(slots=None), I), (dict(k_cache=None), I),
