@@ -5,7 +5,9 @@
  * per sequence, the exact Shannon entropy of the next-token distribution,
  * entropic time and the temperature control law, entropy-driven pruning of
  * the paged KV cache, decode attention over the kept blocks, and sampling at
- * the controlled temperature.
+ * the controlled temperature.  Before it, the prompts: blocks for them,
+ * attention over them, their keys and values into the cache, which may hold
+ * 8-bit codes.
  *
  * Conventions for every entry point:
  *  - Pointers are DEVICE pointers owned by the caller, unless a parameter says
@@ -79,7 +81,8 @@ enum { ENT_SCORE_MEANKEY = 0, ENT_SCORE_EXACT = 1 };
 /* Device-status flags (ent_device_status). */
 #define ENT_DEV_BAD_TABLE 1u     /* a block table entry was out of range */
 #define ENT_DEV_BAD_CTXLEN 2u    /* a context length was out of range */
-#define ENT_DEV_CACHE_FULL 4u    /* append found no room in the block table */
+#define ENT_DEV_CACHE_FULL 4u    /* no room: in the block table (append, plan), or in the
+                                    plan's free list or packed rows */
 
 /* Shapes and control parameters; host values, copied by ent_init.
  * The paper names the control symbols but gives no values (Section 3.3, the
