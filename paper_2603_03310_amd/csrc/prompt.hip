@@ -17,18 +17,22 @@ namespace {
 // workgroup for itself, from 8 B a request (at most 32 KB, in L2 after the
 // first), so one launch does the whole plan: each workgroup then fills its part
 // of the slot map and of the new table entries, the first also writes starts
-// and lengths, and the one that finishes last moves the free list's head,
-// which all have read by then.  Who is last is counted in two steps, each counter
-// in a cache line of its own: counting costs about 10 ns a workgroup and line
-// (1.34M tokens of 256 requests: 14.4 us with 656 workgroups and one counter, 21.1
-// with 1312, 21.5 with their sixteen counters side by side, 9.0 so).
+// and lengths, and the one that is the last to have read the free list's range
+// moves its head.  Who is last is counted in two steps, each counter in a cache
+// line of its own, and the count is taken before the slots and looked at after
+// them: counting costs about 10 ns a workgroup and line (1.34M tokens of 256
+// requests: 14.4 us with 656 workgroups and one counter, 21.1 with 1312, 21.5
+// with their sixteen counters side by side, 9.0 with a line each, 8.4 so).
+//
+// Otherwise a chain of loads, sums and searches bounds it, mostly a launch's own
+// few us: 64 requests that get a token each 4.3 us (5.6 with the counters for a
+// single workgroup too and the free ids loaded where they are written).
 //
 // Requests are admitted in order while tokens and blocks last; the inclusive
 // sums only grow, so "both fit" holds for a prefix of the batch and needs no
 // second pass.
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 256;
-constexpr int kPlanTokens = 1024;      // slots of a workgroup
 constexpr int kPlanCounters = 16;      // counters of finished workgroups, and one over them
 constexpr int kCounterPitch = 32;      // a cache line each
 static_assert((kPlanCounters + 1) * kCounterPitch <= kMinTickets, "counters");
@@ -84,7 +88,23 @@ __device__ __forceinline__ int plan_find(const int* s, int to, int x, int from) 
   return lo;
 }
 
+// The same for one x of a whole wave: 64 places a step.
+__device__ __forceinline__ int plan_find_uniform(const int* s, int to, int x) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = to;
+  while (n > 1) {
+    const int w = (n + 63) / 64;
+    const int k = __popcll(__ballot(lane * w < n && s[lo + min(lane * w, n - 1)] <= x)) - 1;
+    lo += k * w;
+    n = min(w, n - k * w);
+  }
+  return lo;
+}
+
+// kPairs: pairs of slots of a thread.
+template <int kPairs>
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
+  constexpr int kPlanTokens = 2 * kPairs * kPlanThreads;     // slots of a workgroup
   extern __shared__ int s_mem[];
   __shared__ int s_red[2 * kPlanThreads / 64];
   int* s_tok = s_mem;                // [B + 1] packed start of each request
@@ -98,6 +118,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   const int avail = ring_ok ? end - head : 0;
   if (!ring_ok) head = 0;
   unsigned bad = ring_ok ? 0u : ENT_DEV_BAD_TABLE;
+  // The block of this thread's first new table entry, on its way during the sums.
+  const int e0 = blockIdx.x * kPlanThreads + t;
+  const int id0 = e0 < avail ? a.ids[head + e0] : -1;
   // n and ctx of a request; a bad one gets nothing.
   auto request = [&](int b, int& n, int& ctx, unsigned& f) {
     n = a.n_new[b];
@@ -173,15 +196,24 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   }
   __syncthreads();
 
+  // This workgroup has read the free list's range (its threads' `avail`, before the
+  // first barrier).  A counter of one workgroup is not needed.
+  const unsigned n_wg = gridDim.x, c = blockIdx.x % kPlanCounters;
+  const unsigned mine = (n_wg - c + kPlanCounters - 1) / kPlanCounters;       // workgroups of this counter
+  const unsigned used = n_wg < kPlanCounters ? n_wg : kPlanCounters;
+  bool last = t == 0 && ring_ok;
+  unsigned ticket = mine - 1;
+  if (last && mine > 1) ticket = atomicInc(a.tickets + c * kCounterPitch, mine - 1);
+
   const bool pairs = (reinterpret_cast<uintptr_t>(a.slots) & 15) == 0;
   // Slots of this workgroup's tokens, two consecutive ones a thread and step.  The
   // requests that the tokens lie in are found within those of its first and last,
   // mostly one or two; the block ids of all steps are then on their way together.
   const int t0 = blockIdx.x * kPlanTokens;
   const int t1 = min(total, t0 + kPlanTokens);           // tokens from here on are padding
-  constexpr int kPairs = kPlanTokens / (2 * kPlanThreads);
-  const int r0 = t0 < t1 ? plan_find(s_tok, a.B, t0, 0) : 0;
-  const int r1 = t0 < t1 ? plan_find(s_tok, a.B, t1 - 1, r0) + 1 : 0;
+  const bool one = gridDim.x == 1;                       // all of them
+  const int r0 = t0 < t1 && !one ? plan_find_uniform(s_tok, a.B, t0) : 0;
+  const int r1 = t0 < t1 && !one ? plan_find_uniform(s_tok, a.B, t1 - 1) + 1 : a.B;
   int page[2 * kPairs], row[2 * kPairs];
 #pragma unroll
   for (int i = 0; i < 2 * kPairs; ++i) {
@@ -214,10 +246,10 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     }
   }
   // New table entries, dealt to all workgroups.
-  for (int e = blockIdx.x * kPlanThreads + t; e < taken; e += gridDim.x * kPlanThreads) {
+  for (int e = e0; e < taken; e += gridDim.x * kPlanThreads) {
     const int b = plan_find(s_blk, a.B, e, 0);
     const int j = (s_ctx[b] + kBlock - 1) / kBlock + e - s_blk[b];
-    const int p = a.ids[head + e];
+    const int p = e == e0 ? id0 : a.ids[head + e];
     const bool ok = p >= 0 && p < a.P;
     if (!ok) bad |= ENT_DEV_BAD_TABLE;
     a.tables[static_cast<long long>(b) * a.MAXB + j] = ok ? p : -1;
@@ -229,15 +261,10 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     }
   }
   if (bad) raise_flag(a.flags, bad);
-  __syncthreads();
-  if (t == 0 && ring_ok) {
-    const unsigned n = gridDim.x, c = blockIdx.x % kPlanCounters;
-    const unsigned mine = (n - c + kPlanCounters - 1) / kPlanCounters;        // workgroups of this counter
-    const unsigned used = n < kPlanCounters ? n : kPlanCounters;
-    if (atomicInc(a.tickets + c * kCounterPitch, mine - 1) == mine - 1 &&
-        atomicInc(a.tickets + kPlanCounters * kCounterPitch, used - 1) == used - 1)
-      a.range[0] = head + taken;
-  }
+  last = last && ticket == mine - 1;
+  if (last && used > 1)
+    last = atomicInc(a.tickets + kPlanCounters * kCounterPitch, used - 1) == used - 1;
+  if (last) a.range[0] = head + taken;
 }
 
 // ---------------------------------------------------------------------------
@@ -652,9 +679,17 @@ hipError_t launch_prompt_plan(const ent_ctx* c, int B, const int* n_new, const i
   const PlanArgs a{n_new, ctx_lens, tables, free_ids, n_ids, free_range, B,
                    c->cfg.max_blocks_per_seq, c->cfg.num_pool_blocks, max_tokens, starts, slots,
                    new_lens, c->tickets, c->dev_flags};
-  const int grid = std::max(1, (max_tokens + kPlanTokens - 1) / kPlanTokens);
   const size_t lds = static_cast<size_t>(3 * B + 2) * sizeof(int);
-  hipLaunchKernelGGL(plan_kernel, dim3(grid), dim3(kPlanThreads), lds, s, a);
+  // Two slots a thread while that makes four workgroups a CU at most, else four, since
+  // every workgroup forms the sums again.  us with two and with four: one request of 2500
+  // tokens 3.5, 3.9; 64 of 64 4.4, 5.4; 1000 of 300 7.4, 7.6; 256 of 5200 10.1, 8.1.
+  if (max_tokens <= 4 * c->num_cu * 2 * kPlanThreads) {
+    const int grid = std::max(1, (max_tokens + 2 * kPlanThreads - 1) / (2 * kPlanThreads));
+    hipLaunchKernelGGL(plan_kernel<1>, dim3(grid), dim3(kPlanThreads), lds, s, a);
+  } else {
+    const int grid = (max_tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
+    hipLaunchKernelGGL(plan_kernel<2>, dim3(grid), dim3(kPlanThreads), lds, s, a);
+  }
   return hipGetLastError();
 }
 

@@ -80,6 +80,27 @@ def test_plan_largest_batch(torch_cuda):
                          num_q_heads=8, vocab=64), want)
 
 
+@pytest.mark.parametrize("total", [524288, 524289, 700001])
+def test_plan_many_tokens(torch_cuda, total):
+    """Around the number of slots from which a workgroup takes more of them."""
+    rng = np.random.default_rng(total)
+    n = np.full(70, total // 70)
+    n[33] = 0
+    n[-1] += total - n.sum()
+    ctx = rng.integers(0, 40, 70)
+    maxb = int(np.max(-(-(ctx + n) // 16)))
+    have, need = -(-ctx // 16), -(-(ctx + n) // 16) - -(-ctx // 16)
+    P = int(have.sum() + need.sum())
+    ids = rng.permutation(P)
+    tables = np.full((70, maxb), -1)
+    for b in range(70):
+        tables[b, :have[b]] = ids[have[:b].sum():have[:b + 1].sum()]
+    ids = ids[have.sum():]
+    for rows in (total, total - 1):
+        want = OP.plan(n, ctx, tables, ids, [0, len(ids)], rows, P)
+        _same_plan(_run_plan(torch_cuda, n, ctx, tables, ids, [0, len(ids)], rows, P), want)
+
+
 def test_plan_runs_out(torch_cuda):
     """Of blocks, of rows, of both; at the first request, at the last; no free list at all."""
     rng = np.random.default_rng(8)
