@@ -214,6 +214,8 @@ struct AttBf16 {
     struct {
       __attribute__((aligned(256))) uint16_t k[2][BT * D];
       __attribute__((aligned(256))) uint16_t v[2][BT * D];
+      // The queries lie from k[1] on until the first turn; this is what they pass the tiles by.
+      uint16_t over[RG * 32 > 3 * BT ? (RG * 32 - 3 * BT) * D : 8];
     };
     // Partial outputs of the key groups but the first, a column per lane.
     f32x4_t o[KG > 1 ? RG * (KG - 1) : 1][D / 8][64];
@@ -297,18 +299,31 @@ __global__ __launch_bounds__(RG * KG * 64, att_waves(D, KG)) void attend_bf16_ke
   };
 #pragma unroll
   for (int i = 0; i < NL; ++i) load(kp, a.ldk, k_src, 0, k_lds, i);
+  // The queries too, in whole rows, laid out as K's tiles: a lane's own pieces of its row
+  // straight from memory are 16 B here and there: one of 16 tokens 9.7 us so, 8.3 in rows.
+  constexpr int NQ = BM / (WV * RW);
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int row = l_row + i * WV * RW;
+    const uint16_t* p = static_cast<const uint16_t*>(a.q) +
+                        min(t0 + (row >> a.lg), last) * a.ldq + (g * a.G + (row & (a.G - 1))) * D + k_src;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(k_lds + SZ + (wv + i * WV) * RW * D * 2), "v"(p));
+  }
 
   // This lane's row.
   const int r = rg * 32 + r32;
   const bool row_ok = t0 + (r >> a.lg) <= last;
   const int tok = min(t0 + (r >> a.lg), last);
   const int hq = g * a.G + (r & (a.G - 1));
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
   bf16x8_t qf[KS];
   {
-    const uint16_t* p = static_cast<const uint16_t*>(a.q) + tok * a.ldq + hq * D + 8 * h;
+    const int sw = D == 128 ? r & 15 : (r >> 1) & 7;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      uint4 w = *reinterpret_cast<const uint4*>(p + 16 * ks);
+      uint4 w = *reinterpret_cast<const uint4*>(&sh.k[1][r * D + ((2 * ks + h) ^ sw) * 8]);
       w = make_uint4((w.x & a.keep) ^ a.flip, (w.y & a.keep) ^ a.flip, (w.z & a.keep) ^ a.flip,
                      (w.w & a.keep) ^ a.flip);
       qf[ks] = __builtin_bit_cast(bf16x8_t, w);
@@ -480,8 +495,7 @@ __global__ __launch_bounds__(RG * KG * 64, att_waves(D, KG)) void attend_bf16_ke
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (!late) turn();
   };
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  turn();
+  turn();                                 // all have their queries
   if (wv >= WV / 2) half(yes); else half(no);
   __syncthreads();
 
