@@ -257,6 +257,9 @@ __global__ __launch_bounds__(RG * KG * 64, att_waves(D, KG)) void attend_bf16_ke
   // had by what each lane loads.
   const int l_row = wv * RW + lane / CH, l_pos = lane % CH;
   const int k_src = (l_pos ^ (D == 128 ? l_row & 15 : (l_row >> 1) & 7)) * 8;
+  // Load i's row is i WV RW on, which f sees in one bit at most.
+  static_assert((WV * RW) % (D == 128 ? 8 : 16) == 0, "f of a load's rows");
+  auto k_src_of = [&](int i) { return D == 128 && (i * WV * RW & 8) ? k_src ^ 64 : k_src; };
   const int v_src = (l_pos ^ (D == 128 ? (l_row & 3) << 2 : (l_row & 2) << 1)) * 8;
   typedef __attribute__((address_space(3))) char* lds_char;
   auto lds_at = [](const void* p) {
@@ -298,7 +301,7 @@ __global__ __launch_bounds__(RG * KG * 64, att_waves(D, KG)) void attend_bf16_ke
     }
   };
 #pragma unroll
-  for (int i = 0; i < NL; ++i) load(kp, a.ldk, k_src, 0, k_lds, i);
+  for (int i = 0; i < NL; ++i) load(kp, a.ldk, k_src_of(i), 0, k_lds, i);
   // The queries too, in whole rows, laid out as K's tiles: a lane's own pieces of its row
   // straight from memory are 16 B here and there: one of 16 tokens 9.7 us so, 8.3 in rows.
   constexpr int NQ = BM / (WV * RW);
@@ -306,7 +309,7 @@ __global__ __launch_bounds__(RG * KG * 64, att_waves(D, KG)) void attend_bf16_ke
   for (int i = 0; i < NQ; ++i) {
     const int row = l_row + i * WV * RW;
     const uint16_t* p = static_cast<const uint16_t*>(a.q) +
-                        min(t0 + (row >> a.lg), last) * a.ldq + (g * a.G + (row & (a.G - 1))) * D + k_src;
+                        min(t0 + (row >> a.lg), last) * a.ldq + (g * a.G + (row & (a.G - 1))) * D + k_src_of(i);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                  :: "s"(k_lds + SZ + (wv + i * WV) * RW * D * 2), "v"(p));
   }
@@ -458,7 +461,7 @@ __global__ __launch_bounds__(RG * KG * 64, att_waves(D, KG)) void attend_bf16_ke
   // Piece x of what turns 2 j and 2 j + 1 bring: K(j + 1) and V(j).  What they
   // replace, K(j - 1) and V(j - 2), was last read in turn 2 j - 1.
   auto fetch = [&](int j, int x) {
-    if (x < NL) load(kp, a.ldk, k_src, j + 1, k_lds + (j & 1 ? 0 : SZ), x);
+    if (x < NL) load(kp, a.ldk, k_src_of(x), j + 1, k_lds + (j & 1 ? 0 : SZ), x);
     else load(vp, a.ldv, v_src, j, v_lds + (j & 1 ? SZ : 0), x - NL);
   };
   // ... spread over the 2 KB parts of what the half does in turn 2 j.
@@ -772,6 +775,15 @@ hipError_t launch_prompt_attention(const ent_ctx* c, int B, int T, const void* q
            : rg == 2 ? att_launch(attend_f32_kernel<64, 2, 2>, 64, kAttF32Threads, a, s)
                      : att_launch(attend_f32_kernel<64, 1, 4>, 32, kAttF32Threads, a, s);
   }
+  // Short requests (96 tokens on average, padding with them) take what a workgroup costs
+  // beside its tiles, which several small ones on a CU hide for each other.  us with the
+  // rule below and with two waves of 32 rows: one request of 16 tokens (32 / 8 heads of
+  // 128) 8.4, 5.6; 200 of 1 53, 13; 4096 of 1 2180, 810; 512 of 64 214, 205; 300 of 96
+  // 205, 180; 200 of 128 158, 171; 100 of 40 (8 / 8 heads of 64) 15.6, 7.3; but one of
+  // 8000 among 200 of 10 524, 587.
+  if (T <= 96ll * B)
+    return c->cfg.head_dim == 128 ? att_launch(attend_bf16_kernel<128, 2, 1, 32>, 64, 128, a, s)
+                                  : att_launch(attend_bf16_kernel<64, 2, 1, 32>, 64, 128, a, s);
   const int split = rows <= 64 * cus ? 4
                     : rows <= 128 * cus || (rows < 256 * cus && T >= 1024ll * B) ? 2 : 1;
   if (c->cfg.head_dim == 128)

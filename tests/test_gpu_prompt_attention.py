@@ -110,6 +110,15 @@ def test_every_split(torch_cuda):
         _check(*r, "bf16")
 
 
+@pytest.mark.parametrize("heads", [(32, 8, 128), (8, 8, 64), (16, 1, 128), (16, 1, 64), (4, 4, 128)], ids=str)
+def test_short_requests(torch_cuda, heads):
+    """Around the mean length of 96 tokens under which workgroups are small."""
+    for lens in ([96], [97], [1, 191], [2, 191], [95, 97, 96, 0, 192], [0, 400, 1, 1, 0, 65, 64, 63],
+                 [33, 32, 31, 15, 16, 17, 1, 700, 0, 2]):
+        r = _run(torch_cuda, lens, heads, "bf16", seed=sum(lens), pad=sum(lens) % 2)
+        _check(*r, "bf16")
+
+
 def test_every_split_fp32(torch_cuda):
     """The same on either side of the fp32 rules: 24576 and 65536 rows at 256 compute units."""
     for heads, lens in [((8, 8, 64), [1500, 1570]), ((8, 8, 64), [1500, 1571, 2]), ((32, 8, 128), [767]),
