@@ -259,7 +259,9 @@ int ent_block_select(ent_ctx* c, int B, const void* q, const float* ksum, const 
  *   s_i = scale <q_h, k_i>;  out[b, h, :] = sum_i softmax(s)_i v_i;
  *   lse[b, h] = ln sum_i e^{s_i}
  * The softmax is renormalised over the kept tokens.  An empty kept set gives
- * out = 0 and lse = -inf.  out: float [B, H_q, d]; lse (nullable) float [B, H_q]. */
+ * out = 0 and lse = -inf.  A NaN among a valid token's keys or a query's values
+ * gives NaN in the outputs and lse of the heads that read it, a NaN value in its
+ * dim alone.  out: float [B, H_q, d]; lse (nullable) float [B, H_q]. */
 int ent_sparse_paged_decode(ent_ctx* c, int B, const void* q, const void* k_cache,
                             const void* v_cache, const int* block_tables, const int* ctx_lens,
                             const int* kept, const int* n_kept, float* out, float* lse,

@@ -262,6 +262,20 @@ __device__ __forceinline__ s16x4_t load_s16x4(const uint16_t* p) {
 
 constexpr int kSlots = 2 * kWaves;           // cut partials of a workgroup
 
+// A sum of weights is 0 exactly where no token was weighed (its running maximum then
+// still is kLowest); a NaN sum (a NaN among the keys, the query or the scores) is a
+// result like any other and reaches the outputs through every merge, so that what a
+// cut segment gives does not go by where it was cut.  The maxima begin at the lowest
+// finite value: against it a score of -inf weighs 0, against -inf it would weigh NaN.
+constexpr float kLowest = -3.402823466e38f;
+
+// 1 / l, or 0 for the sum of no token.
+__device__ __forceinline__ float inv_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
+// ln of the sum l of weights 2^(s - m).
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
 // The sums of a wave's segment, in the accumulator layout (lane (head r16, gq):
 // dims 16 m + 4 gq .. + 3): to the outputs where its range [u0, u1) holds the
 // whole segment, else to the wave's slot of the workgroup merge.
@@ -282,13 +296,13 @@ __device__ __forceinline__ void flush_segment(const DecodeArgs& a, int cur_seg, 
   if (!head_ok) return;
   if (seg_start >= u0 && seg_end <= u1) {
     const long long oh = static_cast<long long>(b) * Hq + g * G + r16;
-    const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+    const float inv = inv_sum(l_tot);
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       const f32x4_t o = oacc[m] * inv;
       *reinterpret_cast<float4*>(a.out + oh * D + 16 * m + 4 * gq) = make_float4(o[0], o[1], o[2], o[3]);
     }
-    if (gq == 0 && a.lse) a.lse[oh] = l_tot > 0.f ? (m_run + log2f(l_tot)) * kLn2 : -INFINITY;
+    if (gq == 0 && a.lse) a.lse[oh] = lse_of(m_run, l_tot);
   } else {
     // Cut by this wave's range: keep the partial for the workgroup merge.
     const int cs = 2 * wave + (seg_start < u0 ? 0 : 1);
@@ -334,12 +348,12 @@ __device__ __forceinline__ void merge_workgroup(const DecodeArgs& a, int U, int 
     if (seg >= 0 && r < G) {
 #pragma unroll
       for (int kk = 0; kk < kSlots; ++kk)
-        if (s_cseg[kk] == seg && s_cml[(kk * kMaxGroup + r) * 2 + 1] > 0.f)
+        if (s_cseg[kk] == seg && s_cml[(kk * kMaxGroup + r) * 2 + 1] != 0.f)
           M = fmaxf(M, s_cml[(kk * kMaxGroup + r) * 2]);
 #pragma unroll
       for (int kk = 0; kk < kSlots; ++kk) {
         const float l = s_cml[(kk * kMaxGroup + r) * 2 + 1];
-        if (s_cseg[kk] != seg || !(l > 0.f)) continue;
+        if (s_cseg[kk] != seg || l == 0.f) continue;
         const float fk = exp2f(s_cml[(kk * kMaxGroup + r) * 2] - M);
         L += l * fk;
         if (kk == k) f = fk;
@@ -426,10 +440,10 @@ __device__ __forceinline__ void merge_workgroup(const DecodeArgs& a, int U, int 
       const float M = s_wm[i * kMaxGroup + r], L = s_wl[i * kMaxGroup + r];
       if (whole) {
         const long long oh = static_cast<long long>(seg) * G + r;    // b H_q + g G + r
-        const float4 res = L > 0.f ? make_float4(acc.x / L, acc.y / L, acc.z / L, acc.w / L)
-                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 res = L == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                    : make_float4(acc.x / L, acc.y / L, acc.z / L, acc.w / L);
         *reinterpret_cast<float4*>(a.out + oh * D + d) = res;
-        if (d == 0 && a.lse) a.lse[oh] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+        if (d == 0 && a.lse) a.lse[oh] = lse_of(M, L);
       } else {
         *reinterpret_cast<float4*>(a.part_acc + (slot * G + r) * D + d) = acc;
         if (d == 0) {
@@ -512,7 +526,7 @@ __global__ __launch_bounds__(kThreads, 3) void decode_bf16_kernel(DecodeArgs a) 
 
   int cur_seg = -1;
   bf16x8_t qreg[KS];
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = kLowest, l_run = 0.f;
   f32x4_t oacc[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) oacc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -554,7 +568,7 @@ __global__ __launch_bounds__(kThreads, 3) void decode_bf16_kernel(DecodeArgs a) 
         if (head_ok) qreg[ks] = load_bf16x8(q + qh * D + ks * 32 + gq * 8);
         else qreg[ks] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
       }
-      m_run = -INFINITY;
+      m_run = kLowest;
       l_run = 0.f;
 #pragma unroll
       for (int m = 0; m < MT; ++m) oacc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -760,7 +774,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_q8_kernel(DecodeArgs a) {
 
   int cur_seg = -1;
   bf16x8_t qreg[KS];
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = kLowest, l_run = 0.f;
   f32x4_t oacc[MT];
   auto begin_segment = [&](int seg) {
     cur_seg = seg;
@@ -773,7 +787,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_q8_kernel(DecodeArgs a) {
       if (head_ok) qreg[ks] = load_bf16x8(q + qh * D + 64 * (ks / 2) + 16 * gq + 8 * (ks % 2));
       else qreg[ks] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
     }
-    m_run = -INFINITY;
+    m_run = kLowest;
     l_run = 0.f;
 #pragma unroll
     for (int m = 0; m < MT; ++m) oacc[m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -961,11 +975,10 @@ __global__ __launch_bounds__(kThreads) void decode_f32_kernel(DecodeArgs a) {
     for (int h = 0; h < G; ++h) {
       if (whole) {
         const long long oh = static_cast<long long>(b) * Hq + g * G + h;
-        const float inv = l_run[h] > 0.f ? 1.f / l_run[h] : 0.f;
+        const float inv = inv_sum(l_run[h]);
 #pragma unroll
         for (int y = 0; y < DPL; ++y) a.out[oh * D + lane + 64 * y] = o[h][y] * inv;
-        if (lane == 0 && a.lse)
-          a.lse[oh] = l_run[h] > 0.f ? (m_run[h] + log2f(l_run[h])) * kLn2 : -INFINITY;
+        if (lane == 0 && a.lse) a.lse[oh] = lse_of(m_run[h], l_run[h]);
       } else {
 #pragma unroll
         for (int y = 0; y < DPL; ++y) a.part_acc[(slot * G + h) * D + lane + 64 * y] = o[h][y];
@@ -993,7 +1006,7 @@ __global__ __launch_bounds__(kThreads) void decode_f32_kernel(DecodeArgs a) {
       qrow = q + (static_cast<long long>(b) * Hq + g * G) * D + dq * (D / 4);
 #pragma unroll
       for (int h = 0; h < G; ++h) {
-        m_run[h] = -INFINITY;
+        m_run[h] = kLowest;
         l_run[h] = 0.f;
 #pragma unroll
         for (int y = 0; y < DPL; ++y) o[h][y] = 0.f;
@@ -1089,7 +1102,7 @@ inline int few_ranges(int R, int num_cu, int segments) {
 // Running (max, sum, outputs) with a partial or another running triple added.
 __device__ __forceinline__ void combine_add(float& M, float& L, f32x4_t& acc, float m, float l,
                                             f32x4_t v) {
-  if (!(l > 0.f)) return;
+  if (l == 0.f) return;
   const float Mn = fmaxf(M, m);
   const float f_old = (M == -INFINITY) ? 0.f : exp2f(M - Mn);
   const float f_new = exp2f(m - Mn);
@@ -1143,9 +1156,9 @@ __device__ __forceinline__ void combine_body(const DecodeArgs& a, int item) {
     }
   }
   const long long oh = static_cast<long long>(seg) * G + r;    // b H_q + g G + r
-  const f32x4_t res = L > 0.f ? acc / L : f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const f32x4_t res = L == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / L;
   *reinterpret_cast<f32x4_t*>(a.out + oh * D + d) = res;
-  if (d == 0 && a.lse) a.lse[oh] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+  if (d == 0 && a.lse) a.lse[oh] = lse_of(M, L);
 }
 
 template <int D>
