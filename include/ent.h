@@ -355,7 +355,8 @@ int ent_decode_step_append(ent_ctx* c, int B, const float* logits, long long ld,
  * A request that is out of range (negative, or past max_blocks_per_seq blocks)
  * gets nothing and raises ENT_DEV_BAD_CTXLEN or ENT_DEV_CACHE_FULL; a free id or
  * a table entry outside the pool gives slot -1 (and table entry -1) and raises
- * ENT_DEV_BAD_TABLE, as does a free_range outside [0, n_ids], which serves none.
+ * ENT_DEV_BAD_TABLE, as does a free_range outside [0, n_ids], which serves no
+ * request (nor one whose tokens fit the block that it has begun).
  * free_ids must name each block once and none in use.  new_lens and starts must
  * not alias n_new or ctx_lens. */
 int ent_prompt_plan(ent_ctx* c, int B, const int* n_new, const int* ctx_lens, int* block_tables,

@@ -28,9 +28,8 @@ def plan(n_new, ctx_lens, tables, free_ids, free_range, max_tokens: int, num_poo
     ok = 0 <= head <= end <= len(free_ids)
     if not ok:
         flags |= BAD_TABLE
-        end = head
     starts, slots, lens = [0], [], []
-    stop = False
+    stop = not ok                     # a bad range serves nobody, also who needs no block
     at = head
     for b in range(B):
         n, ctx = int(n_new[b]), int(ctx_lens[b])

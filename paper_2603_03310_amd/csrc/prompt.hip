@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   int head = a.range[0];
   const int end = a.range[1];
   const bool ring_ok = head >= 0 && head <= end && end <= a.n_ids;
-  const int avail = ring_ok ? end - head : 0;
+  const int avail = ring_ok ? end - head : -1;         // -1: nobody is served, also who needs no block
   if (!ring_ok) head = 0;
   unsigned bad = ring_ok ? 0u : ENT_DEV_BAD_TABLE;
   // The block of this thread's first new table entry, on its way during the sums.
