@@ -7,7 +7,8 @@
  * the paged KV cache, decode attention over the kept blocks, and sampling at
  * the controlled temperature.  Before it, the prompts: blocks for them,
  * attention over them, their keys and values into the cache, which may hold
- * 8-bit codes.
+ * 8-bit codes.  Around both: queries and keys normalised and turned by their
+ * positions, log probabilities of tokens, and blocks shared, freed and moved.
  *
  * Conventions for every entry point:
  *  - Pointers are DEVICE pointers owned by the caller, unless a parameter says
@@ -81,8 +82,11 @@ enum { ENT_SCORE_MEANKEY = 0, ENT_SCORE_EXACT = 1 };
 /* Device-status flags (ent_device_status). */
 #define ENT_DEV_BAD_TABLE 1u     /* a block table entry was out of range */
 #define ENT_DEV_BAD_CTXLEN 2u    /* a context length was out of range */
-#define ENT_DEV_CACHE_FULL 4u    /* no room: in the block table (append, plan), or in the
-                                    plan's free list or packed rows */
+#define ENT_DEV_CACHE_FULL 4u    /* no room: in the block table (append, plan), in the plan's
+                                    packed rows, or in the free list (plan, fork, release) */
+#define ENT_DEV_BAD_TOKEN 8u     /* a token was past the vocabulary (ent_token_logprobs) */
+#define ENT_DEV_BAD_ROW 16u      /* a row of the tables was out of range or named twice (fork,
+                                    release) */
 
 /* Shapes and control parameters; host values, copied by ent_init.
  * The paper names the control symbols but gives no values (Section 3.3, the
@@ -433,6 +437,115 @@ int ent_sparse_paged_decode_q8(ent_ctx* c, int B, const void* q, const void* k_c
                                const void* v_cache, const float* k_scale, const float* v_scale,
                                const int* block_tables, const int* ctx_lens, const int* kept,
                                const int* n_kept, float* out, float* lse, void* stream);
+
+/* ---- Queries and keys before attention and the cache ---- */
+
+/* Norms and rotation of ent_qk_norm_rope; host struct, device pointers. */
+typedef struct {
+  const float* q_gain;    /* [d] gains of the queries' norm; NULL: queries are not normalised */
+  const float* k_gain;    /* [d] ... of the keys' */
+  const float* inv_freq;  /* [rot_dim / 2] radians per position of each pair (unused when rot_dim is 0) */
+  float eps;              /* added to the mean square, finite and >= 0 */
+  int rot_dim;            /* leading dims of a head that turn: 0 or a multiple of 16, <= d */
+  int adjacent;           /* 0: pairs (i, i + rot_dim / 2); else (2 i, 2 i + 1) */
+} ent_qk_params;
+
+/* Root-mean-square norm of every head of the queries and keys, and the rotation
+ * of its pairs by the token's position, in one pass over T packed rows: for a
+ * head's values x[0 .. d) at position pos
+ *   y_i = x_i gain_i / sqrt((1/d) sum_j x_j^2 + eps)        (y = x without a gain)
+ *   pair (a, b), the i-th:  a' = y_a cos w - y_b sin w,  b' = y_b cos w + y_a sin w,
+ *                           w = pos * inv_freq[i]
+ *   dims from rot_dim on stay y.
+ * Sums in 32 bits, angles in 64 up to the reduction to one turn, outputs rounded
+ * once to kv_dtype; squares must not overflow 32 bits.  Positions: with starts
+ * (int [B + 1], as ent_prompt_plan gives them), row t of request b has position
+ * ctx_lens[b] + t - starts[b], and rows that belong to no request are left as they
+ * are; with starts NULL, T must be B and row b has position ctx_lens[b] (a decode
+ * step's new tokens, before ent_kv_append counts them).  ctx_lens NULL: all 0.  A
+ * request whose ctx_lens is out of range keeps its rows (ENT_DEV_BAD_CTXLEN).
+ * q, k: T rows of H_q d and H_kv d values with strides ldq, ldk (as for
+ * ent_prompt_attention); q_out, k_out likewise.  An output may be its own input
+ * (same pointer and stride); otherwise outputs must not overlap inputs or each
+ * other. */
+int ent_qk_norm_rope(ent_ctx* c, int B, int T, const ent_qk_params* prm, const void* q,
+                     long long ldq, const void* k, long long ldk, const int* starts,
+                     const int* ctx_lens, void* q_out, long long ldqo, void* k_out, long long ldko,
+                     void* stream);
+
+/* ---- Log probabilities of tokens ---- */
+
+/* For each row t < T of logits z (logits_dtype ENT_F32 or ENT_BF16, row stride
+ * ld >= vocab elements), with the softmax p over z / (t_cal temp[t]):
+ *   logprob[t] = ln p(tokens[t]),   entropy[t] = -sum_x p(x) ln p(x),
+ *   top_ids[t, 0 .. n_top), top_logprobs[t, ..]: the n_top likeliest tokens and
+ *   their ln p, largest logit first, equal logits in the order of their index.
+ * temp (nullable): float [T], > 0; NULL: 1.  tokens: int [T]; a negative token
+ * skips its row, which is not read and whose outputs are left as they are; one past
+ * the vocabulary gives logprob NaN (ENT_DEV_BAD_TOKEN).  tokens may be NULL if
+ * logprob is (then no row is skipped); logprob and entropy are nullable, the top
+ * arrays ([T, n_top]) unless n_top is 0.  Logits of -inf have probability 0.  A row
+ * with a NaN or +inf, or with nothing but -inf, has no distribution: its outputs are
+ * NaN and its ids -1.  Sums in 32 bits.  0 <= n_top <= min(vocab,
+ * ENT_MAX_TOP_LOGPROBS); at most ENT_MAX_PACKED_TOKENS rows.  Only the context's
+ * vocab and t_cal matter. */
+#define ENT_MAX_TOP_LOGPROBS 32
+int ent_token_logprobs(ent_ctx* c, int T, const void* logits, int logits_dtype, long long ld,
+                       const int* tokens, const float* temp, float* logprob, float* entropy,
+                       int n_top, int* top_ids, float* top_logprobs, void* stream);
+
+/* ---- Blocks shared, freed and moved ----
+ *
+ * block_tables [R, MAXB] and ctx_lens [R] describe R sequences (R <= max_batch), of
+ * which calls name some by row.  shared (int [num_pool_blocks], zeroed once) counts
+ * for each block the sequences that hold it besides the first; ent_prompt_plan
+ * gives blocks that are not shared, and needs no part in it.  The free list is the
+ * plan's: ids free_ids[free_range[0] .. free_range[1]), taken from the lower end;
+ * blocks go back below it, where the list had those in use.  Only the block that a
+ * sequence is writing (not full) must be its own: forks copy that one and share the
+ * full ones, which no call writes again.
+ * Forks and releases with a free range outside [0, n_ids] change nothing
+ * (ENT_DEV_BAD_TABLE).  A row out of [0, R) is passed over (ENT_DEV_BAD_ROW), a sequence whose length is out of
+ * range too (ENT_DEV_BAD_CTXLEN); a table entry outside the pool is not followed
+ * (ENT_DEV_BAD_TABLE).
+ * k_cache, v_cache: of the context's type; ksum may be NULL in the exact scoring
+ * mode; with k_scale and v_scale (both or
+ * none) the caches hold 8-bit codes, as for the _q8 calls (same conditions).
+ * Caches and ksum need 16-byte alignment. */
+
+/* N forks: row dst[i] becomes a sequence like row src[i]'s, with its full blocks
+ * shared and, where the last one is not full, a block of the free list with its
+ * keys, values, scales and mean keys copied.  dst rows' earlier contents are not
+ * freed.  Free blocks go to the forks in order; the first that finds none, and those
+ * behind it, are passed over and leave their rows alone (ENT_DEV_CACHE_FULL), as is
+ * a fork to a row that an earlier one names as dst, or any names as src
+ * (ENT_DEV_BAD_ROW).  A free id outside the pool gives a table entry of -1
+ * (ENT_DEV_BAD_TABLE).  0 <= N <= R.  src, dst: int [N]. */
+int ent_cache_fork(ent_ctx* c, int N, int R, const int* src, const int* dst, int* block_tables,
+                   int* ctx_lens, int* shared, const int* free_ids, int n_ids, int* free_range,
+                   void* k_cache, void* v_cache, float* k_scale, float* v_scale, float* ksum,
+                   void* stream);
+
+/* The sequences rows[0 .. N) end: ctx_lens[row] becomes 0, and each of their blocks
+ * goes back to the free list, or counts a holder less.  The blocks that become free
+ * stand in ascending order below the list's lower end, which moves down by their
+ * number; where it finds no room the lowest ids are dropped (ENT_DEV_CACHE_FULL).
+ * shared NULL: no block is shared.  A row named twice ends once (ENT_DEV_BAD_ROW); a
+ * block listed more often than shared says is freed once (ENT_DEV_BAD_TABLE).
+ * Tables are left alone.  0 <= N <= R.  rows: int [N]. */
+int ent_cache_release(ent_ctx* c, int N, int R, const int* rows, const int* block_tables,
+                      int* ctx_lens, int* shared, int* free_ids, int n_ids, int* free_range,
+                      void* stream);
+
+/* The U blocks that the R sequences hold move to the pool's lower end: each block
+ * >= U among them, in ascending order, to the free places below U in ascending
+ * order, with its keys, values, scales, mean keys and share count (nullable);
+ * tables follow.  The free list, whatever it held, becomes U .. num_pool_blocks - 1 at the upper end
+ * of free_ids (n_ids >= num_pool_blocks), and *n_used (device int, nullable) U.  A
+ * block that none of the R sequences holds counts as free. */
+int ent_cache_compact(ent_ctx* c, int R, int* block_tables, const int* ctx_lens, int* shared,
+                      int* free_ids, int n_ids, int* free_range, void* k_cache, void* v_cache,
+                      float* k_scale, float* v_scale, float* ksum, int* n_used, void* stream);
 
 /* Entropy-aware scheduling over a pool of N active sequences (Section 3.1:
  * the priority pi(s) = E[Delta H_s] / (alpha C_s + beta M_s + gamma L_s);

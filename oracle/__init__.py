@@ -17,10 +17,13 @@ Modules, each following the paper's definitions (section cited per function):
 * ``append``     -- appending one token to the paged cache.
 * ``schedule``   -- entropy-aware selection of the sequences of the next batch.
 * ``prompt``     -- plans, stores and causal attention of prompts, 8-bit tiles.
+* ``rotate``     -- norms and rotation of queries and keys.
+* ``logprobs``   -- log probabilities, entropy and likeliest tokens of rows.
+* ``pages``      -- blocks of the cache shared, freed and moved.
 * ``layout``     -- reading the library's buffer layouts.
 * ``step``       -- the whole step for a batch, built from the above.
 
 Readings where the paper is silent or garbled are stated in each function's
 docstring; the ones that cannot be pinned to the paper say "parity unpinned".
 """
-from . import entropy, blocks, attention, sample, append, layout, step, schedule, prompt  # noqa: F401
+from . import entropy, blocks, attention, sample, append, layout, step, schedule, prompt, rotate, logprobs, pages  # noqa: F401

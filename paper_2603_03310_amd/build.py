@@ -13,7 +13,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libent.so")
 SOURCES = ["api.hip", "entropy.hip", "blocks.hip", "decode.hip", "step.hip", "prologue.hip", "schedule.hip", "exact.hip", "noalloc.hip",
-           "prompt.hip", "attend.hip"]
+           "prompt.hip", "attend.hip", "rotate.hip", "logprobs.hip", "pages.hip"]
 
 
 def hipcc() -> str:

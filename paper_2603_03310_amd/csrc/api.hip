@@ -136,6 +136,44 @@ int check_store(ent_ctx* c, const char* who, const void* k, long long ldk, const
   return ENT_OK;
 }
 
+// Whether two sets of T rows of n elements, ld apart, touch (T, n >= 1).  Strides that
+// differ: their whole extents.
+bool rows_touch(const void* x, long long ldx, long long nx, const void* y, long long ldy, long long ny,
+                long long T, int elem) {
+  const long long a = static_cast<long long>(reinterpret_cast<uintptr_t>(x)) / elem;
+  const long long b = static_cast<long long>(reinterpret_cast<uintptr_t>(y)) / elem;
+  const long long ax = a + (T - 1) * ldx + nx, bx = b + (T - 1) * ldy + ny;
+  if (ax <= b || bx <= a) return false;
+  if (ldx != ldy) return true;
+  // Row i of x and row j of y: y begins d elements past x, modulo the stride.
+  const long long d = ((b - a) % ldx + ldx) % ldx;
+  return d < nx || d + ny > ldx;
+}
+
+// N of R sequences, and a free list.
+int check_sequences(ent_ctx* c, const char* who, int N, int R, int n_ids) {
+  if (int r = check_device(c)) return r;
+  if (R < 0 || R > c->cfg.max_batch)
+    return fail(c, ENT_E_INVAL, std::string(who) + ": R must be in [0, max_batch]");
+  if (N < 0 || N > R) return fail(c, ENT_E_INVAL, std::string(who) + ": N must be in [0, R]");
+  if (n_ids < 0) return fail(c, ENT_E_INVAL, std::string(who) + ": n_ids must be >= 0");
+  return ENT_OK;
+}
+
+// Caches and scales of the calls that move blocks.
+int check_pages(ent_ctx* c, const char* who, const void* k_cache, const void* v_cache,
+                const float* k_scale, const float* v_scale, const float* ksum) {
+  if (!k_cache || !v_cache || (!ksum && c->cfg.scoring != ENT_SCORE_EXACT))
+    return fail(c, ENT_E_INVAL, std::string(who) + ": NULL required pointer");
+  if (!k_scale != !v_scale)
+    return fail(c, ENT_E_INVAL, std::string(who) + ": k_scale and v_scale go together");
+  if (k_scale)
+    if (int r = check_q8(c, who)) return r;
+  if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(ksum, 16))
+    return fail(c, ENT_E_INVAL, std::string(who) + ": the caches and ksum need 16-byte alignment");
+  return ENT_OK;
+}
+
 size_t align_up(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
@@ -242,9 +280,17 @@ int ent_init(const ent_config* cfg, ent_ctx** out) {
                            ? align_up(Bm * f.max_blocks_per_seq * f.num_q_heads * 2 * sizeof(float))
                            : 0;
   const size_t sz_tick = align_up(std::max(Bm, static_cast<size_t>(ent::kMinTickets)) * sizeof(unsigned));
+  const size_t sz_lps = align_up(ent::kLpSlots * sizeof(float4));
+  const size_t sz_lpk = align_up(ent::kLpSlots * ENT_MAX_TOP_LOGPROBS * sizeof(unsigned long long));
+  const size_t sz_fork = align_up(Bm * sizeof(int4));
+  const size_t words = (static_cast<size_t>(f.num_pool_blocks) + 31) / 32;
+  const size_t sz_pbits = align_up(words * sizeof(unsigned));
+  const size_t sz_psums = align_up(words * sizeof(int2));
+  const size_t sz_pinfo = align_up(2 * sizeof(int));
   const size_t sz_flags = align_up(sizeof(unsigned));
   c->ws_bytes = sz_ent_part + sz_stats + sz_z + sz_lse + sz_lrow + sz_isc + sz_kphys + sz_acc + sz_ml +
-                sz_rec + sz_tmax + sz_ex + sz_tick + sz_flags;
+                sz_rec + sz_tmax + sz_ex + sz_tick + sz_lps + sz_lpk + sz_fork + sz_pbits + sz_psums +
+                sz_pinfo + sz_flags;
   e = hipMalloc(&c->ws, c->ws_bytes);
   if (e != hipSuccess) {
     g_init_error = std::string("workspace allocation failed: ") + hipGetErrorString(e);
@@ -274,6 +320,12 @@ int ent_init(const ent_config* cfg, ent_ctx** out) {
   c->tmax = sz_tmax ? reinterpret_cast<float*>(take(sz_tmax)) : nullptr;
   c->exbuf = sz_ex ? reinterpret_cast<float2*>(take(sz_ex)) : nullptr;
   c->tickets = reinterpret_cast<unsigned*>(take(sz_tick));
+  c->lp_sums = reinterpret_cast<float4*>(take(sz_lps));
+  c->lp_keys = reinterpret_cast<unsigned long long*>(take(sz_lpk));
+  c->fork_rec = reinterpret_cast<int4*>(take(sz_fork));
+  c->page_bits = reinterpret_cast<unsigned*>(take(sz_pbits));
+  c->page_sums = reinterpret_cast<int2*>(take(sz_psums));
+  c->page_info = reinterpret_cast<int*>(take(sz_pinfo));
   c->dev_flags = reinterpret_cast<unsigned*>(take(sz_flags));
   *out = c;
   return ENT_OK;
@@ -611,6 +663,125 @@ int ent_sparse_paged_decode_q8(ent_ctx* c, int B, const void* q, const void* k_c
                                           n_kept, out, lse, static_cast<hipStream_t>(stream), nullptr,
                                           nullptr, nullptr, k_scale, v_scale);
   if (e != hipSuccess) return hip_fail(c, e, "ent_sparse_paged_decode_q8 launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_qk_norm_rope(ent_ctx* c, int B, int T, const ent_qk_params* prm, const void* q,
+                     long long ldq, const void* k, long long ldk, const int* starts,
+                     const int* ctx_lens, void* q_out, long long ldqo, void* k_out, long long ldko,
+                     void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_batch(c, B)) return r;
+  if (int r = check_rows(c, "ent_qk_norm_rope", T)) return r;
+  if (!prm) return fail(c, ENT_E_INVAL, "ent_qk_norm_rope: params is NULL");
+  const ent_qk_params& p = *prm;
+  if (!(p.eps >= 0.f) || !isfinite(p.eps))
+    return fail(c, ENT_E_INVAL, "ent_qk_norm_rope: eps must be finite and >= 0");
+  if (p.rot_dim < 0 || p.rot_dim > c->cfg.head_dim)
+    return fail(c, ENT_E_INVAL, "ent_qk_norm_rope: rot_dim must be in [0, head_dim]");
+  if (p.rot_dim % 16 != 0)
+    return fail(c, ENT_E_UNSUPPORTED, "ent_qk_norm_rope: rot_dim must be a multiple of 16");
+  if (!starts && T != B)
+    return fail(c, ENT_E_INVAL, "ent_qk_norm_rope: without starts, T must be B");
+  if (B == 0 || T == 0) return ENT_OK;
+  if (!q || !k || !q_out || !k_out || (p.rot_dim > 0 && !p.inv_freq))
+    return fail(c, ENT_E_INVAL, "ent_qk_norm_rope: NULL required pointer");
+  const int Hq = c->cfg.num_q_heads, Hkv = c->cfg.num_kv_heads, d = c->cfg.head_dim;
+  if (!row_stride_ok(c, ldq, Hq) || !row_stride_ok(c, ldqo, Hq) || !row_stride_ok(c, ldk, Hkv) ||
+      !row_stride_ok(c, ldko, Hkv))
+    return fail(c, ENT_E_INVAL,
+                "ent_qk_norm_rope: row strides need the row's elements to ENT_MAX_ROW_STRIDE, in 16-byte steps");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16))
+    return fail(c, ENT_E_INVAL, "ent_qk_norm_rope: q, k, q_out and k_out need 16-byte alignment");
+  const int e = c->cfg.kv_dtype == ENT_BF16 ? 2 : 4;
+  const long long nq = static_cast<long long>(Hq) * d, nk = static_cast<long long>(Hkv) * d;
+  const bool q_in_place = q_out == q && ldqo == ldq, k_in_place = k_out == k && ldko == ldk;
+  if ((!q_in_place && rows_touch(q_out, ldqo, nq, q, ldq, nq, T, e)) ||
+      (!k_in_place && rows_touch(k_out, ldko, nk, k, ldk, nk, T, e)) ||
+      rows_touch(q_out, ldqo, nq, k, ldk, nk, T, e) || rows_touch(k_out, ldko, nk, q, ldq, nq, T, e) ||
+      rows_touch(q_out, ldqo, nq, k_out, ldko, nk, T, e))
+    return fail(c, ENT_E_INVAL, "ent_qk_norm_rope: an output overlaps another array");
+  const hipError_t r = ent::launch_qk_norm_rope(c, B, T, p, q, ldq, k, ldk, starts, ctx_lens, q_out, ldqo,
+                                                k_out, ldko, static_cast<hipStream_t>(stream));
+  if (r != hipSuccess) return hip_fail(c, r, "ent_qk_norm_rope launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_token_logprobs(ent_ctx* c, int T, const void* logits, int logits_dtype, long long ld,
+                       const int* tokens, const float* temp, float* logprob, float* entropy,
+                       int n_top, int* top_ids, float* top_logprobs, void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_rows(c, "ent_token_logprobs", T)) return r;
+  if (logits_dtype != ENT_F32 && logits_dtype != ENT_BF16)
+    return fail(c, ENT_E_INVAL, "ent_token_logprobs: logits_dtype must be ENT_F32 or ENT_BF16");
+  if (n_top < 0 || n_top > c->cfg.vocab)
+    return fail(c, ENT_E_INVAL, "ent_token_logprobs: n_top must be in [0, vocab]");
+  if (n_top > ENT_MAX_TOP_LOGPROBS)
+    return fail(c, ENT_E_UNSUPPORTED, "ent_token_logprobs: n_top must be <= ENT_MAX_TOP_LOGPROBS");
+  if (ld < c->cfg.vocab) return fail(c, ENT_E_INVAL, "ent_token_logprobs: ld < vocab");
+  if (T == 0) return ENT_OK;
+  if (!logits || (logprob && !tokens) || (n_top > 0 && (!top_ids || !top_logprobs)))
+    return fail(c, ENT_E_INVAL, "ent_token_logprobs: NULL required pointer");
+  if (!aligned(logits, logits_dtype == ENT_BF16 ? 2 : 4))
+    return fail(c, ENT_E_INVAL, "ent_token_logprobs: logits misaligned");
+  const hipError_t e = ent::launch_token_logprobs(c, T, logits, logits_dtype, ld, tokens, temp, logprob,
+                                                  entropy, n_top, top_ids, top_logprobs,
+                                                  static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(c, e, "ent_token_logprobs launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_cache_fork(ent_ctx* c, int N, int R, const int* src, const int* dst, int* block_tables,
+                   int* ctx_lens, int* shared, const int* free_ids, int n_ids, int* free_range,
+                   void* k_cache, void* v_cache, float* k_scale, float* v_scale, float* ksum,
+                   void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_sequences(c, "ent_cache_fork", N, R, n_ids)) return r;
+  if (N == 0) return ENT_OK;
+  if (!src || !dst || !block_tables || !ctx_lens || !shared || (!free_ids && n_ids > 0) || !free_range)
+    return fail(c, ENT_E_INVAL, "ent_cache_fork: NULL required pointer");
+  if (int r = check_pages(c, "ent_cache_fork", k_cache, v_cache, k_scale, v_scale, ksum)) return r;
+  const hipError_t e = ent::launch_cache_fork(c, N, R, src, dst, block_tables, ctx_lens, shared, free_ids,
+                                              n_ids, free_range, k_cache, v_cache, k_scale, v_scale, ksum,
+                                              static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(c, e, "ent_cache_fork launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_cache_release(ent_ctx* c, int N, int R, const int* rows, const int* block_tables,
+                      int* ctx_lens, int* shared, int* free_ids, int n_ids, int* free_range,
+                      void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_sequences(c, "ent_cache_release", N, R, n_ids)) return r;
+  if (N == 0) return ENT_OK;
+  if (!rows || !block_tables || !ctx_lens || (!free_ids && n_ids > 0) || !free_range)
+    return fail(c, ENT_E_INVAL, "ent_cache_release: NULL required pointer");
+  const hipError_t e = ent::launch_cache_release(c, N, R, rows, block_tables, ctx_lens, shared, free_ids,
+                                                 n_ids, free_range, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(c, e, "ent_cache_release launch");
+  c->err.clear();
+  return ENT_OK;
+}
+
+int ent_cache_compact(ent_ctx* c, int R, int* block_tables, const int* ctx_lens, int* shared,
+                      int* free_ids, int n_ids, int* free_range, void* k_cache, void* v_cache,
+                      float* k_scale, float* v_scale, float* ksum, int* n_used, void* stream) {
+  if (!c) return ENT_E_INVAL;
+  if (int r = check_sequences(c, "ent_cache_compact", 0, R, n_ids)) return r;
+  if (n_ids < c->cfg.num_pool_blocks)
+    return fail(c, ENT_E_INVAL, "ent_cache_compact: free_ids needs room for num_pool_blocks ids");
+  if (R == 0) return ENT_OK;
+  if (!block_tables || !ctx_lens || !free_ids || !free_range)
+    return fail(c, ENT_E_INVAL, "ent_cache_compact: NULL required pointer");
+  if (int r = check_pages(c, "ent_cache_compact", k_cache, v_cache, k_scale, v_scale, ksum)) return r;
+  const hipError_t e = ent::launch_cache_compact(c, R, block_tables, ctx_lens, shared, free_ids, n_ids,
+                                                 free_range, k_cache, v_cache, k_scale, v_scale, ksum,
+                                                 n_used, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(c, e, "ent_cache_compact launch");
   c->err.clear();
   return ENT_OK;
 }

@@ -17,6 +17,7 @@ constexpr int kMaxGroup = 16;               // query heads per KV head
 constexpr int kMinTickets = 1024;           // counters in the workspace, at least
 constexpr int kMaxBlocksPerSeq = 16384;     // selection keeps all scores in LDS
 constexpr int kEstChunkThreads = 256;       // threads of an entropy chunk job (maxima per chunk)
+constexpr int kLpSlots = 1024;              // parts of the rows that log probabilities are cut into
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -83,6 +84,12 @@ struct ent_ctx {
   float2* exbuf = nullptr;        // [max_batch, MAXB, H_q]  exact mode: (log mass, mean logit) per block
   unsigned* tickets = nullptr;    // [max_batch, kMinTickets at least]  counters (zero between launches): per sequence in
                                   // the fused step and the 8-bit append, of workgroups in the prompt plan
+  float4* lp_sums = nullptr;      // [kLpSlots]  sums of parts of rows (log probabilities)
+  unsigned long long* lp_keys = nullptr;   // [kLpSlots, ENT_MAX_TOP_LOGPROBS]  their largest logits
+  int4* fork_rec = nullptr;       // [max_batch]  what each fork does
+  unsigned* page_bits = nullptr;  // [(P + 31) / 32]  a set of blocks (zero between calls)
+  int2* page_sums = nullptr;      // [(P + 31) / 32]  the set again, with its prefix sums
+  int* page_info = nullptr;       // [2]  numbers of used blocks (compact)
   unsigned* dev_flags = nullptr;  // [1]
 
   std::string err;
@@ -232,6 +239,29 @@ hipError_t launch_prompt_attention(const ent_ctx* c, int B, int T, const void* q
                                    const void* k, long long ldk, const void* v, long long ldv,
                                    const int* starts, void* out, long long ldo, float* lse,
                                    hipStream_t s);
+
+// Norms and rotation of queries and keys (rotate.hip).
+hipError_t launch_qk_norm_rope(const ent_ctx* c, int B, int T, const ent_qk_params& p, const void* q,
+                               long long ldq, const void* k, long long ldk, const int* starts,
+                               const int* ctx_lens, void* q_out, long long ldqo, void* k_out,
+                               long long ldko, hipStream_t s);
+// Log probabilities (logprobs.hip).
+hipError_t launch_token_logprobs(const ent_ctx* c, int T, const void* logits, int logits_dtype,
+                                 long long ld, const int* tokens, const float* temp, float* logprob,
+                                 float* entropy, int n_top, int* top_ids, float* top_logprobs,
+                                 hipStream_t s);
+// Blocks shared, freed and moved (pages.hip).
+hipError_t launch_cache_fork(const ent_ctx* c, int N, int R, const int* src, const int* dst,
+                             int* tables, int* ctx_lens, int* shared, const int* free_ids, int n_ids,
+                             int* free_range, void* k_cache, void* v_cache, float* k_scale,
+                             float* v_scale, float* ksum, hipStream_t s);
+hipError_t launch_cache_release(const ent_ctx* c, int N, int R, const int* rows, const int* tables,
+                                int* ctx_lens, int* shared, int* free_ids, int n_ids,
+                                int* free_range, hipStream_t s);
+hipError_t launch_cache_compact(const ent_ctx* c, int R, int* tables, const int* ctx_lens, int* shared,
+                                int* free_ids, int n_ids, int* free_range, void* k_cache,
+                                void* v_cache, float* k_scale, float* v_scale, float* ksum,
+                                int* n_used, hipStream_t s);
 
 // Configuration check of ent_init (message, ENT_OK / ENT_E_INVAL /
 // ENT_E_UNSUPPORTED in *code), and the message ent_last_error(NULL) returns

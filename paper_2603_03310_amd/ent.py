@@ -23,6 +23,8 @@ ENT_SCORE_MEANKEY, ENT_SCORE_EXACT = 0, 1
 ENT_ROW_CHUNK = 4096
 ENT_BLOCK_SIZE = 16
 ENT_DEV_BAD_TABLE, ENT_DEV_BAD_CTXLEN, ENT_DEV_CACHE_FULL = 1, 2, 4
+ENT_DEV_BAD_TOKEN, ENT_DEV_BAD_ROW = 8, 16
+ENT_MAX_TOP_LOGPROBS = 32
 
 EXPORTED = ("ent_default_config", "ent_check_config", "ent_row_stats_chunks", "ent_init",
             "ent_destroy", "ent_last_error", "ent_device_status", "ent_entropy_temperature",
@@ -30,7 +32,8 @@ EXPORTED = ("ent_default_config", "ent_check_config", "ent_row_stats_chunks", "e
             "ent_kv_append", "ent_decode_step", "ent_schedule", "ent_entropy_temperature_noalloc",
             "ent_decode_step_append", "ent_prompt_plan", "ent_prompt_store",
             "ent_prompt_store_q8", "ent_prompt_attention", "ent_kv_append_q8",
-            "ent_sparse_paged_decode_q8")
+            "ent_sparse_paged_decode_q8", "ent_qk_norm_rope", "ent_token_logprobs",
+            "ent_cache_fork", "ent_cache_release", "ent_cache_compact")
 ENT_MAX_PACKED_TOKENS, ENT_MAX_ROW_STRIDE = 1 << 21, 1 << 24
 ENT_NOALLOC_SCRATCH_BYTES = 2 << 20
 ENT_SCHED_MAX_POOL = 8192
@@ -61,6 +64,13 @@ class ent_sched_params(ctypes.Structure):
 class ent_state(ctypes.Structure):
     _fields_ = [("h_prev", ctypes.c_void_p), ("tau", ctypes.c_void_p), ("temp", ctypes.c_void_p),
                 ("kappa", ctypes.c_void_p)]
+
+
+class ent_qk_params(ctypes.Structure):
+    """Device addresses: the tensors have to outlive the calls (make_qk_params keeps them)."""
+    _fields_ = [("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p),
+                ("inv_freq", ctypes.c_void_p), ("eps", ctypes.c_float), ("rot_dim", ctypes.c_int),
+                ("adjacent", ctypes.c_int)]
 
 
 class EntError(RuntimeError):
@@ -111,6 +121,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "ent_prompt_attention": (i, [vp, i, i, vp, ll, vp, ll, vp, ll, vp, vp, ll, vp, vp]),
         "ent_kv_append_q8": (i, [vp, i] + [vp] * 10),
         "ent_sparse_paged_decode_q8": (i, [vp, i] + [vp] * 12),
+        "ent_qk_norm_rope": (i, [vp, i, i, ctypes.POINTER(ent_qk_params), vp, ll, vp, ll, vp, vp, vp,
+                                 ll, vp, ll, vp]),
+        "ent_token_logprobs": (i, [vp, i, vp, i, ll, vp, vp, vp, vp, i, vp, vp, vp]),
+        "ent_cache_fork": (i, [vp, i, i] + [vp] * 6 + [i] + [vp] * 7),
+        "ent_cache_release": (i, [vp, i, i] + [vp] * 5 + [i, vp, vp]),
+        "ent_cache_compact": (i, [vp, i] + [vp] * 4 + [i] + [vp] * 8),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -299,3 +315,47 @@ def ent_sparse_paged_decode_q8(ctx, B, q, k_cache, v_cache, k_scale, v_scale, bl
                                                   ptr(k_scale), ptr(v_scale), ptr(block_tables),
                                                   ptr(ctx_lens), ptr(kept), ptr(n_kept), ptr(out),
                                                   ptr(lse), _stream(stream)))
+
+
+def make_qk_params(q_gain, k_gain, inv_freq, eps, rot_dim, adjacent=False) -> ent_qk_params:
+    """Parameters of ent_qk_norm_rope from float32 device tensors (gains None: no norm)."""
+    p = ent_qk_params(ptr(q_gain), ptr(k_gain), ptr(inv_freq), eps, rot_dim, int(adjacent))
+    p.tensors = (q_gain, k_gain, inv_freq)
+    return p
+
+
+def ent_qk_norm_rope(ctx, B, T, prm: ent_qk_params, q, ldq, k, ldk, starts, ctx_lens, q_out, ldqo,
+                     k_out, ldko, stream=None):
+    _check(ctx, load().ent_qk_norm_rope(ctx, B, T, ctypes.byref(prm), ptr(q), ldq, ptr(k), ldk,
+                                        ptr(starts), ptr(ctx_lens), ptr(q_out), ldqo, ptr(k_out),
+                                        ldko, _stream(stream)))
+
+
+def ent_token_logprobs(ctx, T, logits, logits_dtype, ld, tokens, temp, logprob, entropy, n_top=0,
+                       top_ids=None, top_logprobs=None, stream=None):
+    _check(ctx, load().ent_token_logprobs(ctx, T, ptr(logits), logits_dtype, ld, ptr(tokens), ptr(temp),
+                                          ptr(logprob), ptr(entropy), n_top, ptr(top_ids),
+                                          ptr(top_logprobs), _stream(stream)))
+
+
+def ent_cache_fork(ctx, N, R, src, dst, block_tables, ctx_lens, shared, free_ids, n_ids, free_range,
+                   k_cache, v_cache, k_scale, v_scale, ksum, stream=None):
+    _check(ctx, load().ent_cache_fork(ctx, N, R, ptr(src), ptr(dst), ptr(block_tables), ptr(ctx_lens),
+                                      ptr(shared), ptr(free_ids), n_ids, ptr(free_range), ptr(k_cache),
+                                      ptr(v_cache), ptr(k_scale), ptr(v_scale), ptr(ksum),
+                                      _stream(stream)))
+
+
+def ent_cache_release(ctx, N, R, rows, block_tables, ctx_lens, shared, free_ids, n_ids, free_range,
+                      stream=None):
+    _check(ctx, load().ent_cache_release(ctx, N, R, ptr(rows), ptr(block_tables), ptr(ctx_lens),
+                                         ptr(shared), ptr(free_ids), n_ids, ptr(free_range),
+                                         _stream(stream)))
+
+
+def ent_cache_compact(ctx, R, block_tables, ctx_lens, shared, free_ids, n_ids, free_range, k_cache,
+                      v_cache, k_scale, v_scale, ksum, n_used=None, stream=None):
+    _check(ctx, load().ent_cache_compact(ctx, R, ptr(block_tables), ptr(ctx_lens), ptr(shared),
+                                         ptr(free_ids), n_ids, ptr(free_range), ptr(k_cache),
+                                         ptr(v_cache), ptr(k_scale), ptr(v_scale), ptr(ksum),
+                                         ptr(n_used), _stream(stream)))

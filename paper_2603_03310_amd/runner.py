@@ -23,7 +23,9 @@ class Decoder:
     the caches hold 8-bit codes: `step` then runs the four calls (with
     ent_sparse_paged_decode_q8), `store` and `append` the 8-bit forms.  `plan`,
     `store` and `prompt` bring a batch of packed prompts into the cache and attend
-    over them."""
+    over them.  `rotate` normalises and turns queries and keys before that,
+    `logprobs` scores tokens, and `fork`, `release` and `compact` share, free and
+    move the cache's blocks."""
 
     def __init__(self, **fields):
         self.cfg = make_config(**fields)
@@ -97,6 +99,44 @@ class Decoder:
         T, Hq, Hkv = q.shape[0], self.cfg.num_q_heads, self.cfg.num_kv_heads
         ldq, ldk, ldv, ldo = (self._rows(x, T, H) for x, H in ((q, Hq), (k, Hkv), (v, Hkv), (out, Hq)))
         ent.ent_prompt_attention(self.ctx, B, T, q, ldq, k, ldk, v, ldv, starts, out, ldo, lse, stream)
+
+    def rotate(self, B, prm, q, k, q_out, k_out, starts=None, ctx_lens=None, stream=None):
+        """Norms and rotation of rows q, q_out [T, H_q, d] and k, k_out [T, H_kv, d] (outputs may be
+        the inputs); without starts, row b is sequence b's next token."""
+        T, Hq, Hkv = q.shape[0], self.cfg.num_q_heads, self.cfg.num_kv_heads
+        ldq, ldk, ldqo, ldko = (self._rows(x, T, H) for x, H in ((q, Hq), (k, Hkv), (q_out, Hq), (k_out, Hkv)))
+        ent.ent_qk_norm_rope(self.ctx, B, T, prm, q, ldq, k, ldk, starts, ctx_lens, q_out, ldqo, k_out,
+                             ldko, stream)
+
+    def logprobs(self, logits, tokens, logprob, entropy=None, top_ids=None, top_logprobs=None, temp=None,
+                 stream=None):
+        """Log probabilities of tokens [T] under logits [T, vocab] (float32 or bfloat16)."""
+        import torch
+        kinds = {torch.float32: ent.ENT_F32, torch.bfloat16: ent.ENT_BF16}
+        if logits.dtype not in kinds or logits.stride(1) != 1:
+            raise ent.EntError(ent.ENT_E_INVAL, "logits: float32 or bfloat16 rows in one piece needed")
+        n_top = 0 if top_ids is None else top_ids.shape[1]
+        ent.ent_token_logprobs(self.ctx, logits.shape[0], logits, kinds[logits.dtype], logits.stride(0),
+                               tokens, temp, logprob, entropy, n_top, top_ids, top_logprobs, stream)
+
+    def fork(self, src, dst, block_tables, ctx_lens, shared, free_ids, free_range, k_cache, v_cache, ksum,
+             k_scale=None, v_scale=None, stream=None):
+        """Rows dst become sequences like rows src, whose full blocks they share."""
+        ent.ent_cache_fork(self.ctx, src.numel(), ctx_lens.numel(), src, dst, block_tables, ctx_lens, shared,
+                           free_ids, free_ids.numel(), free_range, k_cache, v_cache, k_scale, v_scale, ksum,
+                           stream)
+
+    def release(self, rows, block_tables, ctx_lens, free_ids, free_range, shared=None, stream=None):
+        """The sequences of these rows end; blocks that nobody holds go back to the free list."""
+        ent.ent_cache_release(self.ctx, rows.numel(), ctx_lens.numel(), rows, block_tables, ctx_lens, shared,
+                              free_ids, free_ids.numel(), free_range, stream)
+
+    def compact(self, block_tables, ctx_lens, free_ids, free_range, k_cache, v_cache, ksum, shared=None,
+                k_scale=None, v_scale=None, n_used=None, stream=None):
+        """All blocks in use to the pool's lower end."""
+        ent.ent_cache_compact(self.ctx, ctx_lens.numel(), block_tables, ctx_lens, shared, free_ids,
+                              free_ids.numel(), free_range, k_cache, v_cache, k_scale, v_scale, ksum, n_used,
+                              stream)
 
     def _rows(self, x, T, heads):
         """The row stride of T packed rows of whole heads, side by side."""
