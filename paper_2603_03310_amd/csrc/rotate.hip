@@ -5,9 +5,8 @@
 // 32 lanes hold a head (sum of squares by cross-lane adds), so a lane holds the
 // same dims of every head that it sees and forms its cosines and sines once.  With
 // gains g and pairs (a, b) of inverse root r,
-//   a' = r (x_a g_a cos - x_b g_b sin),  b' = r (x_b g_b cos + x_a g_a sin):
-// out_i = r (x_i A_i + x_p B_i) with A_i = g_i cos, B_i = -+ g_p sin per lane.
-// Pairs (i, i + rot / 2) lie rot / 2 dims apart, a whole number of lanes.
+//   a' = r (x_a g_a cos - x_b g_b sin),  b' = r (x_b g_b cos + x_a g_a sin).
+// Pairs (i, i + rot / 2) lie a whole number of lanes apart.
 
 #include "ent_internal.h"
 
@@ -19,6 +18,7 @@ namespace ent {
 namespace {
 
 constexpr int kRotThreads = 256;
+constexpr int kRotWaves = 8192;       // waves that few rows are cut into
 
 struct RotArgs {
   const void* src[2];     // queries, keys
@@ -51,64 +51,85 @@ __device__ __forceinline__ int find_request(const int* s, int n, int x) {
   return lo;
 }
 
+// 16 bytes of a row as N floats.
 template <typename T>
-struct Piece;
-template <>
-struct Piece<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ void load(const float* p, float (&x)[4]) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-  }
-  static __device__ __forceinline__ void store(float* p, const float (&x)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  }
-};
-template <>
-struct Piece<uint16_t> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void load(const uint16_t* p, float (&x)[8]) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
+struct Piece {
+  static constexpr int N = 16 / sizeof(T);
+  static __device__ __forceinline__ void widen(uint4 v, float (&x)[N]) {
     const unsigned w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      if constexpr (N == 4) {
+        x[i] = __uint_as_float(w[i]);
+      } else {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
     }
   }
-  static __device__ __forceinline__ void store(uint16_t* p, const float (&x)[8]) {
+  static __device__ __forceinline__ uint4 narrow(const float (&x)[N]) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     unsigned w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      bf16x2 b;
-      b[0] = static_cast<__bf16>(x[2 * i]);
-      b[1] = static_cast<__bf16>(x[2 * i + 1]);
-      w[i] = __builtin_bit_cast(unsigned, b);
+      if constexpr (N == 4) {
+        w[i] = __float_as_uint(x[i]);
+      } else {
+        bf16x2 b;
+        b[0] = static_cast<__bf16>(x[2 * i]);
+        b[1] = static_cast<__bf16>(x[2 * i + 1]);
+        w[i] = __builtin_bit_cast(unsigned, b);
+      }
     }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
 };
 
-template <typename T, int D>
+// Which lane holds a lane's pairs' other dims: itself (adjacent pairs), the lane half a
+// head away (all dims turn in pairs of halves), or some other.
+enum { kAdjacent, kHalves, kAnyHalves };
+
+template <typename T, int D, int PAIRS>
 __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
   using P = Piece<T>;
   constexpr int N = P::N;
   constexpr int L = D / N;                 // lanes of a head
   constexpr int H = 64 / L;                // heads of a wave's step
+  constexpr int U = 3;                     // steps whose loads are in flight together
   const int lane = threadIdx.x & 63, l = lane % L;
-  const long long w = static_cast<long long>(blockIdx.x) * (kRotThreads / 64) + (threadIdx.x >> 6);
-  const int row = static_cast<int>(w / a.parts), part = static_cast<int>(w % a.parts);
+  const unsigned w = blockIdx.x * (kRotThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned parts = a.parts;
+  const int row = static_cast<int>(w / parts), part = static_cast<int>(w - row * parts);
   if (row >= a.T) return;
+  const int sq = (a.heads[0] + H - 1) / H, steps = sq + (a.heads[1] + H - 1) / H;
+  const int s0 = part * steps / static_cast<int>(parts), s1 = (part + 1) * steps / static_cast<int>(parts);
+  const int dim0 = l * N;
+  const T* const src0 = static_cast<const T*>(a.src[0]) + row * a.ld_src[0];
+  const T* const src1 = static_cast<const T*>(a.src[1]) + row * a.ld_src[1];
+  // This lane's place in step s; past the last head, the last head again.
+  auto place = [&](int s, bool& keys, bool& ok) {
+    keys = s >= sq;
+    const int h = (keys ? s - sq : s) * H + lane / L, heads = a.heads[keys ? 1 : 0];
+    ok = h < heads;
+    return min(h, heads - 1) * D + dim0;
+  };
+  auto fetch = [&](int s) {
+    bool keys, ok;
+    const int at = place(s, keys, ok);
+    return *reinterpret_cast<const uint4*>((keys ? src1 : src0) + at);
+  };
+  uint4 raw[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) raw[u] = fetch(min(s0 + u, s1 - 1));
   long long pos;
   {
     int b = row;
     long long at = 0;
     if (a.starts) {
       b = find_request(a.starts, a.B, row);
-      const int s0 = a.starts[b];
-      if (row < s0 || row >= a.starts[b + 1]) return;
-      at = static_cast<long long>(row) - s0;
+      const int first = a.starts[b];
+      if (row < first || row >= a.starts[b + 1]) return;
+      at = static_cast<long long>(row) - first;
     }
     const int n = a.ctx ? a.ctx[b] : 0;
     if (n < 0 || n > a.room) {
@@ -117,48 +138,76 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
     }
     pos = n + at;
   }
-  float cs[N], sn[N];
   const int half = a.rot / 2;
-  const int dim0 = l * N;
-  const bool turns = dim0 < a.rot;         // rot is a multiple of 16: all dims of a lane or none
-  const bool second = !a.adjacent && dim0 >= half;
+  const bool turns = PAIRS == kHalves || dim0 < a.rot;     // rot is a multiple of 16: all dims of a lane or none
+  const bool second = PAIRS != kAdjacent && dim0 >= half;
+  auto angle = [&](int i, float& c, float& s) {
+    // In half turns, reduced to [-1, 1] in 64 bits.
+    const double t = static_cast<double>(pos) * (static_cast<double>(a.freq[i]) * 0.31830988618379067154);
+    sincospif(static_cast<float>(t - 2.0 * rint(0.5 * t)), &s, &c);
+  };
+  float cs[N], sn[N];
+  if constexpr (PAIRS == kAdjacent) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    cs[j] = 1.f;
-    sn[j] = 0.f;
-    if (turns) {
-      const int i = a.adjacent ? (dim0 + j) / 2 : dim0 + j - (second ? half : 0);
-      // In half turns, reduced to [-1, 1] in 64 bits.
-      const double t = static_cast<double>(pos) * (static_cast<double>(a.freq[i]) * 0.31830988618379067154);
-      float s, c;
-      sincospif(static_cast<float>(t - 2.0 * rint(0.5 * t)), &s, &c);
-      cs[j] = c;
-      const bool up = a.adjacent ? (j & 1) : second;
-      sn[j] = up ? s : -s;
+    for (int j = 0; j < N; j += 2) {
+      float c = 1.f, s = 0.f;
+      if (turns) angle((dim0 + j) / 2, c, s);
+      cs[j] = cs[j + 1] = c;
+      sn[j] = -s;
+      sn[j + 1] = s;
     }
-  }
-  const int mate = a.adjacent || !turns ? lane : (second ? lane - half / N : lane + half / N);
-  for (int which = 0; which < 2; ++which) {
-    const T* src = static_cast<const T*>(a.src[which]) + static_cast<long long>(row) * a.ld_src[which];
-    T* dst = static_cast<T*>(a.dst[which]) + static_cast<long long>(row) * a.ld_dst[which];
-    const float* g = a.gain[which];
-    float A[N], B[N];
+  } else if constexpr (PAIRS == kHalves) {
+    // The two lanes of a pair form half of its angles each.
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+      float c, s;
+      angle(dim0 - (second ? half - N / 2 : 0) + j, c, s);
+      const float oc = __uint_as_float(xor_lane<L / 2>(__float_as_uint(c)));
+      const float os = __uint_as_float(xor_lane<L / 2>(__float_as_uint(s)));
+      cs[j] = second ? oc : c;
+      cs[j + N / 2] = second ? c : oc;
+      sn[j] = second ? os : -s;
+      sn[j + N / 2] = second ? s : -os;
+    }
+  } else {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int d = dim0 + j;
-      const int p = a.adjacent ? (d ^ 1) : turns ? (second ? d - half : d + half) : d;
-      A[j] = cs[j] * (g ? g[d] : 1.f);
-      B[j] = sn[j] * (g ? g[p] : 1.f);
+      float c = 1.f, s = 0.f;
+      if (turns) angle(dim0 + j - (second ? half : 0), c, s);
+      cs[j] = c;
+      sn[j] = second ? s : -s;
     }
-    const int heads = a.heads[which];
-    for (int h0 = part * H; h0 < heads; h0 += a.parts * H) {
-      const int h = h0 + lane / L;
-      const bool ok = h < heads;
-      const int off = min(h, heads - 1) * D + dim0;
+  }
+  const int mate = PAIRS != kAnyHalves || !turns ? lane : second ? lane - half / N : lane + half / N;
+  float g[N];
+  bool norm = false;
+  int kind = -1;                           // whose gains g holds
+  T* const dst0 = static_cast<T*>(a.dst[0]) + row * a.ld_dst[0];
+  T* const dst1 = static_cast<T*>(a.dst[1]) + row * a.ld_dst[1];
+  for (int s = s0; s < s1; s += U) {
+    uint4 now[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) now[u] = raw[u];
+    if (s + U < s1) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = fetch(min(s + U + u, s1 - 1));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s + u >= s1) break;
+      bool keys, ok;
+      const int at = place(s + u, keys, ok);
+      if (kind != (keys ? 1 : 0)) {
+        kind = keys ? 1 : 0;
+        const float* gain = a.gain[kind];
+        norm = gain != nullptr;
+#pragma unroll
+        for (int j = 0; j < N; ++j) g[j] = norm ? gain[dim0 + j] : 1.f;
+      }
       float x[N], y[N];
-      P::load(src + off, x);
+      P::widen(now[u], x);
       float r = 1.f;
-      if (g) {
+      if (norm) {
         float ss = 0.f;
 #pragma unroll
         for (int j = 0; j < N; ++j) ss = fmaf(x[j], x[j], ss);
@@ -168,19 +217,26 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
         if constexpr (L >= 16) ss = xor_add<8>(ss);
         if constexpr (L >= 32) ss = xor_add<16>(ss);
         r = rsqrtf(fmaf(ss, 1.f / D, a.eps));
-      }
-      if (!turns) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) y[j] = r * (x[j] * A[j]);
+        for (int j = 0; j < N; ++j) x[j] *= g[j];
       }
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const float m = a.adjacent ? x[j ^ 1] : __shfl(x[j], mate);
-        if (turns) y[j] = r * fmaf(x[j], A[j], m * B[j]);
+        float m;                           // the pair's other
+        if constexpr (PAIRS == kAdjacent) m = x[j ^ 1];
+        else if constexpr (PAIRS == kHalves) m = __uint_as_float(xor_lane<L / 2>(__float_as_uint(x[j])));
+        else m = __shfl(x[j], mate);
+        y[j] = r * (turns ? fmaf(x[j], cs[j], m * sn[j]) : x[j]);
       }
-      if (ok) P::store(dst + off, y);
+      if (ok) *reinterpret_cast<uint4*>((keys ? dst1 : dst0) + at) = P::narrow(y);
     }
   }
+}
+
+template <typename T, int D>
+auto rotate_for(int pairs) {
+  return pairs == kAdjacent ? rotate_kernel<T, D, kAdjacent>
+         : pairs == kHalves ? rotate_kernel<T, D, kHalves> : rotate_kernel<T, D, kAnyHalves>;
 }
 
 }  // namespace
@@ -207,12 +263,16 @@ hipError_t launch_qk_norm_rope(const ent_ctx* c, int B, int T, const ent_qk_para
   a.T = T;
   a.room = f.max_blocks_per_seq * kBlock;
   a.flags = c->dev_flags;
-  a.parts = 4;
+  const bool bf16 = f.kv_dtype == ENT_BF16;
+  // Waves of a row: where rows are few, as many as it has steps.
+  const int per = 64 * (bf16 ? 8 : 4) / f.head_dim;
+  const int steps = (f.num_q_heads + per - 1) / per + (f.num_kv_heads + per - 1) / per;
+  a.parts = std::max(1, std::min(steps, kRotWaves / T));
   const long long waves = static_cast<long long>(T) * a.parts;
   const dim3 grid(static_cast<unsigned>((waves + kRotThreads / 64 - 1) / (kRotThreads / 64)));
-  const bool bf16 = f.kv_dtype == ENT_BF16;
-  auto kern = bf16 ? (f.head_dim == 64 ? rotate_kernel<uint16_t, 64> : rotate_kernel<uint16_t, 128>)
-                   : (f.head_dim == 64 ? rotate_kernel<float, 64> : rotate_kernel<float, 128>);
+  const int pairs = a.adjacent ? kAdjacent : a.rot == f.head_dim ? kHalves : kAnyHalves;
+  auto kern = bf16 ? (f.head_dim == 64 ? rotate_for<uint16_t, 64>(pairs) : rotate_for<uint16_t, 128>(pairs))
+                   : (f.head_dim == 64 ? rotate_for<float, 64>(pairs) : rotate_for<float, 128>(pairs));
   hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), 0, s, a);
   return hipGetLastError();
 }
