@@ -121,6 +121,26 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
   uint4 raw[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) raw[u] = fetch(min(s0 + u, s1 - 1));
+  // The lane's gains and frequencies are on their way before its position is known.
+  const int half = a.rot / 2;
+  const bool turns = PAIRS == kHalves || dim0 < a.rot;     // rot is a multiple of 16: all dims of a lane or none
+  const bool second = PAIRS != kAdjacent && dim0 >= half;
+  constexpr int F = PAIRS == kAnyHalves ? N : N / 2;       // angles that a lane forms
+  const int f0 = PAIRS == kAdjacent ? dim0 / 2
+                 : PAIRS == kHalves ? dim0 - (second ? half - N / 2 : 0) : dim0 - (second ? half : 0);
+  float freq[F];
+#pragma unroll
+  for (int j = 0; j < F; ++j) freq[j] = turns ? a.freq[f0 + j] : 0.f;
+  float g[N];
+  bool norm;
+  auto gains = [&](int which) {
+    const float* gain = a.gain[which];
+    norm = gain != nullptr;
+#pragma unroll
+    for (int j = 0; j < N; ++j) g[j] = norm ? gain[dim0 + j] : 1.f;
+  };
+  int kind = s0 >= sq ? 1 : 0;             // whose gains g holds
+  gains(kind);
   long long pos;
   {
     int b = row;
@@ -138,50 +158,34 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
     }
     pos = n + at;
   }
-  const int half = a.rot / 2;
-  const bool turns = PAIRS == kHalves || dim0 < a.rot;     // rot is a multiple of 16: all dims of a lane or none
-  const bool second = PAIRS != kAdjacent && dim0 >= half;
-  auto angle = [&](int i, float& c, float& s) {
+  auto angle = [&](int j, float& c, float& s) {
     // In half turns, reduced to [-1, 1] in 64 bits.
-    const double t = static_cast<double>(pos) * (static_cast<double>(a.freq[i]) * 0.31830988618379067154);
+    const double t = static_cast<double>(pos) * (static_cast<double>(freq[j]) * 0.31830988618379067154);
     sincospif(static_cast<float>(t - 2.0 * rint(0.5 * t)), &s, &c);
   };
-  float cs[N], sn[N];
-  if constexpr (PAIRS == kAdjacent) {
+  float cs[N], sn[N];                      // dims that do not turn: frequency 0
 #pragma unroll
-    for (int j = 0; j < N; j += 2) {
-      float c = 1.f, s = 0.f;
-      if (turns) angle((dim0 + j) / 2, c, s);
-      cs[j] = cs[j + 1] = c;
-      sn[j] = -s;
-      sn[j + 1] = s;
-    }
-  } else if constexpr (PAIRS == kHalves) {
-    // The two lanes of a pair form half of its angles each.
-#pragma unroll
-    for (int j = 0; j < N / 2; ++j) {
-      float c, s;
-      angle(dim0 - (second ? half - N / 2 : 0) + j, c, s);
+  for (int j = 0; j < F; ++j) {
+    float c, s;
+    angle(j, c, s);
+    if constexpr (PAIRS == kAdjacent) {
+      cs[2 * j] = cs[2 * j + 1] = c;
+      sn[2 * j] = -s;
+      sn[2 * j + 1] = s;
+    } else if constexpr (PAIRS == kHalves) {
+      // The two lanes of a pair form half of its angles each.
       const float oc = __uint_as_float(xor_lane<L / 2>(__float_as_uint(c)));
       const float os = __uint_as_float(xor_lane<L / 2>(__float_as_uint(s)));
       cs[j] = second ? oc : c;
-      cs[j + N / 2] = second ? c : oc;
+      cs[j + F] = second ? c : oc;
       sn[j] = second ? os : -s;
-      sn[j + N / 2] = second ? s : -os;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      float c = 1.f, s = 0.f;
-      if (turns) angle(dim0 + j - (second ? half : 0), c, s);
+      sn[j + F] = second ? s : -os;
+    } else {
       cs[j] = c;
       sn[j] = second ? s : -s;
     }
   }
   const int mate = PAIRS != kAnyHalves || !turns ? lane : second ? lane - half / N : lane + half / N;
-  float g[N];
-  bool norm = false;
-  int kind = -1;                           // whose gains g holds
   T* const dst0 = static_cast<T*>(a.dst[0]) + row * a.ld_dst[0];
   T* const dst1 = static_cast<T*>(a.dst[1]) + row * a.ld_dst[1];
   for (int s = s0; s < s1; s += U) {
@@ -197,13 +201,7 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
       if (s + u >= s1) break;
       bool keys, ok;
       const int at = place(s + u, keys, ok);
-      if (kind != (keys ? 1 : 0)) {
-        kind = keys ? 1 : 0;
-        const float* gain = a.gain[kind];
-        norm = gain != nullptr;
-#pragma unroll
-        for (int j = 0; j < N; ++j) g[j] = norm ? gain[dim0 + j] : 1.f;
-      }
+      if (kind != (keys ? 1 : 0)) gains(kind = keys ? 1 : 0);
       float x[N], y[N];
       P::widen(now[u], x);
       float r = 1.f;
