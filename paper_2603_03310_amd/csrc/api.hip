@@ -280,8 +280,9 @@ int ent_init(const ent_config* cfg, ent_ctx** out) {
                            ? align_up(Bm * f.max_blocks_per_seq * f.num_q_heads * 2 * sizeof(float))
                            : 0;
   const size_t sz_tick = align_up(std::max(Bm, static_cast<size_t>(ent::kMinTickets)) * sizeof(unsigned));
-  const size_t sz_lps = align_up(ent::kLpSlots * sizeof(float4));
+  const size_t sz_lps = align_up(ent::kLpSlots * 3 * sizeof(float));
   const size_t sz_lpk = align_up(ent::kLpSlots * ENT_MAX_TOP_LOGPROBS * sizeof(unsigned long long));
+  const size_t sz_lpt = align_up(ent::kLpSlots / 2 * sizeof(unsigned));
   const size_t sz_fork = align_up(Bm * sizeof(int4));
   const size_t words = (static_cast<size_t>(f.num_pool_blocks) + 31) / 32;
   const size_t sz_pbits = align_up(words * sizeof(unsigned));
@@ -289,7 +290,7 @@ int ent_init(const ent_config* cfg, ent_ctx** out) {
   const size_t sz_pinfo = align_up(2 * sizeof(int));
   const size_t sz_flags = align_up(sizeof(unsigned));
   c->ws_bytes = sz_ent_part + sz_stats + sz_z + sz_lse + sz_lrow + sz_isc + sz_kphys + sz_acc + sz_ml +
-                sz_rec + sz_tmax + sz_ex + sz_tick + sz_lps + sz_lpk + sz_fork + sz_pbits + sz_psums +
+                sz_rec + sz_tmax + sz_ex + sz_tick + sz_lps + sz_lpk + sz_lpt + sz_fork + sz_pbits + sz_psums +
                 sz_pinfo + sz_flags;
   e = hipMalloc(&c->ws, c->ws_bytes);
   if (e != hipSuccess) {
@@ -320,8 +321,9 @@ int ent_init(const ent_config* cfg, ent_ctx** out) {
   c->tmax = sz_tmax ? reinterpret_cast<float*>(take(sz_tmax)) : nullptr;
   c->exbuf = sz_ex ? reinterpret_cast<float2*>(take(sz_ex)) : nullptr;
   c->tickets = reinterpret_cast<unsigned*>(take(sz_tick));
-  c->lp_sums = reinterpret_cast<float4*>(take(sz_lps));
+  c->lp_sums = reinterpret_cast<float*>(take(sz_lps));
   c->lp_keys = reinterpret_cast<unsigned long long*>(take(sz_lpk));
+  c->lp_tickets = reinterpret_cast<unsigned*>(take(sz_lpt));
   c->fork_rec = reinterpret_cast<int4*>(take(sz_fork));
   c->page_bits = reinterpret_cast<unsigned*>(take(sz_pbits));
   c->page_sums = reinterpret_cast<int2*>(take(sz_psums));

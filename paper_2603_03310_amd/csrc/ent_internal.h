@@ -84,7 +84,8 @@ struct ent_ctx {
   float2* exbuf = nullptr;        // [max_batch, MAXB, H_q]  exact mode: (log mass, mean logit) per block
   unsigned* tickets = nullptr;    // [max_batch, kMinTickets at least]  counters (zero between launches): per sequence in
                                   // the fused step and the 8-bit append, of workgroups in the prompt plan
-  float4* lp_sums = nullptr;      // [kLpSlots]  sums of parts of rows (log probabilities)
+  float* lp_sums = nullptr;       // [kLpSlots, 3]  sums of parts of rows (log probabilities)
+  unsigned* lp_tickets = nullptr; // [kLpSlots / 2]  finished parts of rows (zero between launches)
   unsigned long long* lp_keys = nullptr;   // [kLpSlots, ENT_MAX_TOP_LOGPROBS]  their largest logits
   int4* fork_rec = nullptr;       // [max_batch]  what each fork does
   unsigned* page_bits = nullptr;  // [(P + 31) / 32]  a set of blocks (zero between calls)

@@ -6,14 +6,20 @@
 //   ln p(x) = ln 2 (c (z_x - M) - log2 S),   H = ln 2 (log2 S - c W / S).
 // (The difference comes first, so rows of the type's lowest value overflow nothing.)
 // A thread walks the 16-byte pieces of its row (or of its part of it) that lie a
-// workgroup's width apart, and keeps its own maximum, sums, and the piece where its
-// maximum first stood.  Of all threads the n with the largest (maximum, then
-// earliest piece) hold the n largest logits between them: were one elsewhere, its
-// thread's maximum would be among the n.  Only their pieces are read again, and of
-// those only values at or above the n-th such maximum count, mostly little more
-// than n, which are ranked by counting.
+// workgroup's width apart, and keeps its own maximum, sums, the piece where its
+// maximum first stood, and its maximum in each of eight segments of the walk.  Of all
+// threads the n with the largest (maximum, then earliest piece) hold the n largest
+// logits between them: were one elsewhere, its thread's maximum would be among the n.
+// A bound that those n reach (and some more threads: it comes from a bisection by
+// ballots over one wave's registers, which ends where it lets through enough and not
+// many more) names the segments of theirs that have to be read again, and of those
+// only values that reach it count, mostly little more than n, which are ranked by
+// counting.  (A piece is alone in its cache line for its thread: without the segments,
+// 33 threads' walks for n = 20 are as much traffic as the row.)
 //
-// Few rows are cut into parts; a second launch joins their sums and lists.
+// Few rows are cut into parts, each with a list of its n largest; the workgroup that
+// finishes a row's last part joins them.  What it reads of the others was written
+// through device-scope stores that had completed before the row's ticket was drawn.
 
 #include "ent_internal.h"
 
@@ -27,7 +33,16 @@ namespace {
 constexpr int kLpThreads = 256;
 constexpr int kLpTop = ENT_MAX_TOP_LOGPROBS;
 constexpr int kLpCand = 1024;         // candidates that are ranked at once
-constexpr int kLpUnroll = 4;
+constexpr int kLpParts = 64;          // parts of a row, at most
+constexpr int kLpWho = 64;            // threads that can reach the bound
+constexpr int kLpSegs = 8;            // segments of a thread's walk
+static_assert(kLpTop * kLpTop <= kLpCand, "keys of a row's n lists");
+static_assert(kLpTop + kLpTop / 2 + 3 <= kLpWho, "threads over the bound");
+static_assert(kLpParts == 64 && kLpParts <= kLpThreads, "a wave joins the parts");
+constexpr int kLpUnroll = 4;          // pieces of a thread in flight
+// Logits past what the last-level cache holds are read without a place in the caches:
+// 2500 rows of 128256 floats 238 us against 257 with; 64 rows of bf16 18.8 against 18.4.
+constexpr long long kLpStream = 256ll << 20;
 typedef unsigned long long u64;
 
 struct LpArgs {
@@ -41,8 +56,9 @@ struct LpArgs {
   float* entropy;         // nullable
   int* top_ids;
   float* top_lp;
-  float4* sums;           // [T * parts]  (max, S, W) of parts
+  float* sums;            // [T * parts, 3]  (max, S, W) of parts
   u64* keys;              // [T * parts, n_top]  their largest logits, descending
+  unsigned* tickets;      // [T]  finished parts, 0 between launches
   unsigned* flags;
 };
 
@@ -60,7 +76,7 @@ __device__ __forceinline__ u64 lp_key(float x, int i) {
 
 // A row's 16-byte pieces: piece p holds the elements [p N - shift, p N - shift + N)
 // that lie in [0, V), so that pieces are aligned whatever the row's start.
-template <typename T>
+template <typename T, bool STREAM>
 struct Row {
   static constexpr int N = 16 / sizeof(T);
   const T* base;     // the row's first element
@@ -83,7 +99,10 @@ struct Row {
   }
   __device__ __forceinline__ bool whole(int p) const { return p * N >= shift && (p + 1) * N - shift <= V; }
   __device__ __forceinline__ uint4 raw(int p) const {
-    return *reinterpret_cast<const uint4*>(base + (static_cast<long long>(p) * N - shift));
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4* q = reinterpret_cast<const u32x4*>(base + (static_cast<long long>(p) * N - shift));
+    const u32x4 v = STREAM ? __builtin_nontemporal_load(q) : *q;
+    return make_uint4(v.x, v.y, v.z, v.w);
   }
   // Any piece; elements outside the row read as -inf.
   __device__ __forceinline__ void load(int p, float (&x)[N]) const {
@@ -132,149 +151,161 @@ __device__ __forceinline__ void lp_write_top(const LpArgs& a, int row, int i, u6
   a.top_lp[o] = ((x - m) * c - l) * kLn2;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs a) {
-  constexpr int N = Row<T>::N, NT = kLpThreads, U = kLpUnroll;
-  __shared__ u64 s_key[NT];
-  __shared__ u64 s_cand[kLpCand];
-  __shared__ float s_red[3 * NT / 64];
-  __shared__ int s_who[kLpTop];
-  __shared__ u64 s_edge;
-  __shared__ int s_count;
-  __shared__ float s_ml[2];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-  const int tok = a.tokens ? a.tokens[row] : 0;
-  if (tok < 0) return;
-  const LpScale sc(a, row);
-  const T* base = static_cast<const T*>(a.logits) + static_cast<long long>(row) * a.ld;
-  const Row<T> r(base, a.V);
-  const int np = r.pieces();
-  const int p0 = static_cast<int>(static_cast<long long>(np) * part / a.parts);
-  const int p1 = static_cast<int>(static_cast<long long>(np) * (part + 1) / a.parts);
-  const float z = a.logprob && tok < a.V ? Row<T>::value(base[tok]) : 0.f;
+// Values that another workgroup of the launch reads.
+template <typename V>
+__device__ __forceinline__ void lp_share(V* p, V v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename V>
+__device__ __forceinline__ V lp_shared(const V* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
-  float mx = -INFINITY, s = 0.f, w = 0.f;
-  int mp = p0 + t;                         // first piece that holds mx
-  auto take = [&](const float (&x)[N], int p) {
-    float b = x[0];
+struct LpShared {
+  u64 key[kLpThreads];       // per thread: its largest logit (of its maxima, first piece)
+  u64 cand[kLpCand];
+  float red[3 * kLpThreads / 64];
+  float seg[kLpSegs][kLpThreads];   // ... in each segment
+  int again[kLpWho * kLpSegs];      // (segment, thread) that are read again
+  u64 edge;
+  int count, agains, last;
+  float ml[2];
+};
+
+// A bound that at least n of a wave's keys (K a lane, distinct but for 0, which is none)
+// reach, and at most `most` >= n of them: by bisection, first over the upper words, then,
+// where too many share the n-th's, over the lower words of those.  All keys but 0 where
+// they are no more than `most`, and anything where they are fewer than n.
+template <int K>
+__device__ __forceinline__ u64 lp_bound(const u64 (&key)[K], int n, int most) {
+  unsigned hi[K], top = 0u, least = 0xffffffffu;
+  int there = 0;
 #pragma unroll
-    for (int j = 1; j < N; ++j) b = fmaxf(b, x[j]);
-    if (b > mx) {
-      const LpSums q = lp_to(LpSums{mx, s, w}, b, sc);
-      s = q.s;
-      w = q.w;
-      mx = b;
-      mp = p;
-    }
-    const float from = mx == -INFINITY ? 0.f : mx;
+  for (int k = 0; k < K; ++k) {
+    hi[k] = static_cast<unsigned>(key[k] >> 32);
+    top = max(top, hi[k]);
+    if (key[k] != 0ull) least = min(least, hi[k]);
+    there += static_cast<int>(__popcll(__ballot(key[k] != 0ull)));
+  }
+  if (there <= most) return there < n ? 1ull : static_cast<u64>(wave_min_u(least)) << 32;
+  auto count = [&](unsigned from) {
+    int c = 0;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float d = x[j] - from;
-      const float e = __builtin_amdgcn_exp2f(d * sc.c);
-      s += e;
-      w = fmaf(e, fmaxf(d, sc.low), w);      // e is 0 there; NaN stays in s
-    }
+    for (int k = 0; k < K; ++k) c += static_cast<int>(__popcll(__ballot(hi[k] >= from)));
+    return c;
   };
-  for (int p = p0 + t; p < p1; p += U * NT) {
-    float x[U][N];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (p + u * NT < p1) r.load(p + u * NT, x[u]);
-      else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[u][j] = -INFINITY;
-      }
+  // All keys but 0 reach `lo`, which grows while n do; fewer than n reach `end`.  Where
+  // no lane is empty, each lane's largest reaches the least of them.
+  unsigned lo = max(wave_min_u(top), 1u), end = wave_max_u(top) + 1u;
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  end = __builtin_amdgcn_readfirstlane(end);
+  int c = count(lo);
+  while (c > most && end - lo > 1u) {
+    const unsigned mid = lo + (end - lo) / 2u;
+    const int m = count(mid);
+    if (m >= n) {
+      lo = mid;
+      c = m;
+    } else {
+      end = mid;
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) take(x[u], p + u * NT);
   }
+  if (c <= most) return static_cast<u64>(lo) << 32;
+  // Too many at lo itself: the largest lower words among them.
+  const int need = n - count(lo + 1u);
+  auto ties = [&](unsigned from) {
+    int t = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      t += static_cast<int>(__popcll(__ballot(hi[k] == lo && static_cast<unsigned>(key[k]) >= from)));
+    return t;
+  };
+  unsigned first = 0xffffffffu, last = 0u;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (hi[k] == lo) {
+      first = min(first, static_cast<unsigned>(key[k]));
+      last = max(last, static_cast<unsigned>(key[k]));
+    }
+  }
+  unsigned low = wave_min_u(first), past = wave_max_u(last);   // at least `need` reach low
+  low = __builtin_amdgcn_readfirstlane(low);
+  past = __builtin_amdgcn_readfirstlane(past);
+  if (ties(past) >= need) return static_cast<u64>(lo) << 32 | past;
+  while (past - low > 1u) {
+    const unsigned mid = low + (past - low) / 2u;
+    if (ties(mid) >= need) low = mid;
+    else past = mid;
+  }
+  return static_cast<u64>(lo) << 32 | low;
+}
 
-  // Sums of the workgroup.
-  LpSums g{mx, s, w};
-  {
-    const float m = wave_max(g.m);
-    g = lp_to(g, m, sc);
-    g.s = wave_sum(g.s);
-    g.w = wave_sum(g.w);
-    if (lane == 0) {
-      s_red[3 * wave] = g.m;
-      s_red[3 * wave + 1] = g.s;
-      s_red[3 * wave + 2] = g.w;
-    }
-    s_key[t] = p0 + t < p1 ? lp_key(mx, mp) : 0ull;
-    if (t == 0) {
-      s_count = 0;
-      s_edge = 0ull;
-    }
-    __syncthreads();
-    float mm = s_red[0];
-#pragma unroll
-    for (int i = 1; i < NT / 64; ++i) mm = fmaxf(mm, s_red[3 * i]);
-    float ss = 0.f, sw = 0.f;
-#pragma unroll
-    for (int i = 0; i < NT / 64; ++i) {
-      const LpSums q = lp_to(LpSums{s_red[3 * i], s_red[3 * i + 1], s_red[3 * i + 2]}, mm, sc);
-      ss += q.s;
-      sw += q.w;
-    }
-    g = LpSums{mm, ss, sw};
-  }
-  const bool whole = a.parts == 1;
-  if (t == 0) {
-    if (whole) lp_outputs(a, row, g, sc.c, tok, z, s_ml[0], s_ml[1]);
-    else a.sums[blockIdx.x] = make_float4(g.m, g.s, g.w, 0.f);
-  }
-  const int n = a.n_top;
-  if (n == 0) return;
-
-  // The n threads with the largest keys, and the n-th key.
-  {
-    const u64 mine = s_key[t];
+// The n largest of sh.cand[0 .. cand) by counting: f(rank, key).
+template <typename F>
+__device__ __forceinline__ void lp_rank(const LpShared& sh, int cand, int n, F f) {
+  for (int i = threadIdx.x; i < cand; i += kLpThreads) {
+    const u64 mine = sh.cand[i];
     int rank = 0;
-    for (int i = 0; i < NT; ++i) rank += s_key[i] > mine ? 1 : 0;
-    if (mine != 0ull && rank < n) {
-      s_who[rank] = t;
-      if (rank == n - 1) s_edge = mine;
-    }
+    for (int k = 0; k < cand; ++k) rank += sh.cand[k] > mine ? 1 : 0;
+    if (rank < n) f(rank, mine);
   }
-  const int who = min(n, min(NT, max(p1 - p0, 0)));
+}
+
+// The n largest logits of pieces [p0, p1), `per` pieces of a thread in a segment, given
+// the threads' largest in sh.key and sh.seg.
+template <typename R>
+__device__ __forceinline__ void lp_largest(const LpArgs& a, LpShared& sh, const R& r, int p0, int p1, int per,
+                                           int row, float c) {
+  constexpr int N = R::N, NT = kLpThreads;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, n = a.n_top;
+  const bool whole = a.parts == 1;
+  auto put = [&](int rank, u64 key) {
+    if (whole) lp_write_top(a, row, rank, key, c, sh.ml[0], sh.ml[1]);
+    else lp_share(a.keys + static_cast<long long>(blockIdx.x) * n + rank, key);
+  };
+  // Threads whose largest logits are among the n largest of the threads', and some more.
+  if (wave == 0) {
+    u64 key[NT / 64];
+#pragma unroll
+    for (int k = 0; k < NT / 64; ++k) key[k] = sh.key[k * 64 + lane];
+    const u64 e = lp_bound(key, n, n + n / 2 + 3);
+    if (lane == 0) sh.edge = e;
+  }
   __syncthreads();
-  const u64 edge = s_edge;
-  const float ev = lp_value(static_cast<unsigned>(edge >> 32));
-  const int ep = static_cast<int>(~static_cast<unsigned>(edge));
+  const u64 edge = sh.edge;
+  const unsigned eo = static_cast<unsigned>(edge >> 32);
+  const int ep = static_cast<unsigned>(edge) == 0u || eo == 0u ? 0x7fffffff : static_cast<int>(~static_cast<unsigned>(edge));
+  if (sh.key[t] >= edge) {
+#pragma unroll
+    for (int g = 0; g < kLpSegs; ++g)
+      if (p0 + t + g * per * NT < p1 && lp_order(sh.seg[g][t]) >= eo) sh.again[atomicAdd(&sh.agains, 1)] = g * NT + t;
+  }
+  __syncthreads();
+  const int units = sh.agains * per;
   // Whether element (x, i) of piece p can be among the n largest.
   auto counts = [&](float x, int i, int p) {
-    return i >= 0 && i < a.V && (edge == 0ull || x > ev || (x == ev && p <= ep));
+    const unsigned o = lp_order(x);
+    return i >= 0 && i < a.V && x == x && (o > eo || (o == eo && p <= ep));
   };
-  for (int k = wave; k < who; k += NT / 64) {
-    const int first = p0 + s_who[k];
-    for (int p = first + lane * NT; p < p1; p += 64 * NT) {
+  for (int u = t; u < units; u += NT) {
+    const int w = sh.again[u / per], p = p0 + w % NT + (w / NT * per + u % per) * NT;
+    if (p < p1) {
       float x[N];
       r.load(p, x);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const int i = p * N + j - r.shift;
         if (counts(x[j], i, p)) {
-          const int at = atomicAdd(&s_count, 1);
-          if (at < kLpCand) s_cand[at] = lp_key(x[j], i);
+          const int at = atomicAdd(&sh.count, 1);
+          if (at < kLpCand) sh.cand[at] = lp_key(x[j], i);
         }
       }
     }
   }
   __syncthreads();
-  const int cand = s_count;
-  auto put = [&](int rank, u64 key) {
-    if (whole) lp_write_top(a, row, rank, key, sc.c, s_ml[0], s_ml[1]);
-    else a.keys[static_cast<long long>(blockIdx.x) * n + rank] = key;
-  };
+  const int cand = sh.count;
   if (cand <= kLpCand) {
-    for (int i = t; i < cand; i += NT) {
-      const u64 mine = s_cand[i];
-      int rank = 0;
-      for (int k = 0; k < cand; ++k) rank += s_cand[k] > mine ? 1 : 0;
-      if (rank < n) put(rank, mine);
-    }
+    lp_rank(sh, cand, n, put);
     // A part shorter than n, or a row with NaN.
     for (int i = cand + t; i < n; i += NT) put(i, 0ull);
     return;
@@ -297,51 +328,184 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs a) {
       }
     }
     __syncthreads();
-    s_key[t] = best;
+    sh.key[t] = best;
     __syncthreads();
     best = 0ull;
-    for (int i = 0; i < NT; ++i) best = s_key[i] > best ? s_key[i] : best;
+    for (int i = 0; i < NT; ++i) best = sh.key[i] > best ? sh.key[i] : best;
     if (t == 0) put(k, best);
     last = best;
   }
 }
 
-// One wave a row: the parts' sums, and the n largest of their descending lists.
-__global__ __launch_bounds__(64) void logprobs_join_kernel(LpArgs a, int logits_bf16) {
-  __shared__ u64 s_key[64 * kLpTop];
-  const int row = blockIdx.x, lane = threadIdx.x, n = a.n_top;
+// A row's outputs from its parts' sums and descending lists, by one workgroup.  A bound
+// that n keys reach: the n-th largest of the lists' first keys, or, of fewer lists, the
+// least of their q-th, where q entries of each are n.
+__device__ __forceinline__ void lp_join(const LpArgs& a, LpShared& sh, int row, const LpScale& sc, int tok,
+                                        float z) {
+  constexpr int NT = kLpThreads, K = kLpParts * kLpTop / NT;
+  const int t = threadIdx.x, n = a.n_top, total = a.parts * n;
+  const long long first = static_cast<long long>(row) * a.parts;
+  const u64* keys = a.keys + first * n;
+  u64 mine[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) mine[k] = t + k * NT < total ? lp_shared(keys + t + k * NT) : 0ull;
+  if (t < 64) {
+    LpSums g{-INFINITY, 0.f, 0.f};
+    u64 head = 0ull;                       // of the list, or its q-th key
+    const int q = n == 0 ? 1 : (n + a.parts - 1) / a.parts;
+    if (t < a.parts) {
+      const float* o = a.sums + 3 * (first + t);
+      g = LpSums{lp_shared(o), lp_shared(o + 1), lp_shared(o + 2)};
+      if (n > 0) head = lp_shared(keys + static_cast<long long>(t) * n + q - 1);
+    }
+    g = lp_to(g, wave_max(g.m), sc);
+    g.s = wave_sum(g.s);
+    g.w = wave_sum(g.w);
+    if (t == 0) {
+      lp_outputs(a, row, g, sc.c, tok, z, sh.ml[0], sh.ml[1]);
+      sh.count = 0;
+    }
+    if (n > 0) {
+      u64 e;
+      if (q == 1) {
+        const u64 one[1] = {head};
+        e = lp_bound(one, n, n);
+      } else {
+        const u64 mine = t < a.parts ? head : ~0ull;
+        const unsigned hi = wave_min_u(static_cast<unsigned>(mine >> 32));
+        e = static_cast<u64>(hi) << 32;    // the keys of this logit, all of them
+      }
+      if (t == 0) sh.edge = e;
+    }
+  }
+  if (n == 0) return;
+  __syncthreads();
+  const u64 edge = sh.edge;
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (mine[k] != 0ull && mine[k] >= edge) {
+      const int at = atomicAdd(&sh.count, 1);
+      if (at < kLpCand) sh.cand[at] = mine[k];
+    }
+  __syncthreads();
+  const int cand = min(sh.count, kLpCand);
+  auto put = [&](int rank, u64 key) { lp_write_top(a, row, rank, key, sc.c, sh.ml[0], sh.ml[1]); };
+  lp_rank(sh, cand, n, put);
+  for (int i = cand + t; i < n; i += NT) put(i, 0ull);         // a row with NaN
+}
+
+template <typename T, bool STREAM>
+__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs a) {
+  using R = Row<T, STREAM>;
+  constexpr int N = R::N, NT = kLpThreads, U = kLpUnroll;
+  __shared__ LpShared sh;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
   const int tok = a.tokens ? a.tokens[row] : 0;
   if (tok < 0) return;
   const LpScale sc(a, row);
-  const long long at = static_cast<long long>(row) * a.ld + tok;
-  float z = 0.f;
-  if (a.logprob && tok < a.V)
-    z = logits_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.logits)[at]) : static_cast<const float*>(a.logits)[at];
-  const long long first = static_cast<long long>(row) * a.parts;
-  LpSums g{-INFINITY, 0.f, 0.f};
-  if (lane < a.parts) {
-    const float4 v = a.sums[first + lane];
-    g = LpSums{v.x, v.y, v.z};
+  const T* base = static_cast<const T*>(a.logits) + static_cast<long long>(row) * a.ld;
+  const R r(base, a.V);
+  const int np = r.pieces();
+  const int p0 = static_cast<int>(static_cast<long long>(np) * part / a.parts);
+  const int p1 = static_cast<int>(static_cast<long long>(np) * (part + 1) / a.parts);
+  const float z = a.logprob && tok < a.V ? R::value(base[tok]) : 0.f;
+
+  float mx = -INFINITY, s = 0.f, w = 0.f;
+  int mp = p0 + t;                         // first piece that holds mx
+  auto take = [&](const float (&x)[N], int p) {
+    float b = x[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) b = fmaxf(b, x[j]);
+    if (b > mx) {
+      const LpSums q = lp_to(LpSums{mx, s, w}, b, sc);
+      s = q.s;
+      w = q.w;
+      mx = b;
+      mp = p;
+    }
+    const float from = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float d = x[j] - from;
+      const float e = __builtin_amdgcn_exp2f(d * sc.c);
+      s += e;
+      w = fmaf(e, fmaxf(d, sc.low), w);      // e is 0 there; NaN stays in s
+    }
+    return b;
+  };
+  // The walk, in segments of `rounds` steps.
+  const int rounds = (p1 - p0 + U * NT * kLpSegs - 1) / (U * NT * kLpSegs);
+  for (int g = 0, p = p0 + t; p - t < p1; ++g) {
+    float top = -INFINITY;
+    for (int k = 0; k < rounds; ++k, p += U * NT) {
+      float x[U][N];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p + u * NT < p1) r.load(p + u * NT, x[u]);
+        else {
+#pragma unroll
+          for (int j = 0; j < N; ++j) x[u][j] = -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) top = fmaxf(top, take(x[u], p + u * NT));
+    }
+    sh.seg[g][t] = top;
   }
-  for (int i = lane; i < a.parts * n; i += 64) s_key[i] = a.keys[first * n + i];
-  g = lp_to(g, wave_max(g.m), sc);
-  g.s = wave_sum(g.s);
-  g.w = wave_sum(g.w);
-  float m = 0.f, l = 0.f;
-  if (lane == 0) lp_outputs(a, row, g, sc.c, tok, z, m, l);
-  m = lane_at(m, 0);
-  l = lane_at(l, 0);
+
+  // Sums of the workgroup.
+  LpSums g{mx, s, w};
+  {
+    const float m = wave_max(g.m);
+    g = lp_to(g, m, sc);
+    g.s = wave_sum(g.s);
+    g.w = wave_sum(g.w);
+    if (lane == 0) {
+      sh.red[3 * wave] = g.m;
+      sh.red[3 * wave + 1] = g.s;
+      sh.red[3 * wave + 2] = g.w;
+    }
+    sh.key[t] = p0 + t < p1 ? lp_key(mx, mp) : 0ull;
+    if (t == 0) sh.count = sh.agains = 0;
+    __syncthreads();
+    float mm = sh.red[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) mm = fmaxf(mm, sh.red[3 * i]);
+    float ss = 0.f, sw = 0.f;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) {
+      const LpSums q = lp_to(LpSums{sh.red[3 * i], sh.red[3 * i + 1], sh.red[3 * i + 2]}, mm, sc);
+      ss += q.s;
+      sw += q.w;
+    }
+    g = LpSums{mm, ss, sw};
+  }
+  const bool whole = a.parts == 1;
+  if (t == 0) {
+    if (whole) {
+      lp_outputs(a, row, g, sc.c, tok, z, sh.ml[0], sh.ml[1]);
+    } else {
+      float* o = a.sums + 3 * blockIdx.x;
+      lp_share(o, g.m);
+      lp_share(o + 1, g.s);
+      lp_share(o + 2, g.w);
+    }
+  }
+  const int n = a.n_top;
+  if (n > 0) lp_largest(a, sh, r, p0, p1, rounds * U, row, sc.c);
+  if (whole) return;
+
+  // The row's last part joins them all.
+  __builtin_amdgcn_s_waitcnt(0);         // this wave's device-scope stores have completed
   __syncthreads();
-  int next = 0;
-  for (int k = 0; k < n; ++k) {
-    const u64 head = lane < a.parts && next < n ? s_key[lane * n + next] : 0ull;
-    const unsigned hi = static_cast<unsigned>(head >> 32), lo = static_cast<unsigned>(head);
-    const unsigned top = wave_max_u(hi);
-    const unsigned low = wave_max_u(hi == top ? lo : 0u);
-    const u64 best = static_cast<u64>(top) << 32 | low;
-    if (head == best) ++next;              // keys differ, but for 0
-    if (lane == 0) lp_write_top(a, row, k, best, sc.c, m, l);
-  }
+  if (t == 0)
+    sh.last = __hip_atomic_fetch_add(a.tickets + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+              static_cast<unsigned>(a.parts) - 1u;
+  __syncthreads();
+  if (!sh.last) return;
+  if (t == 0) a.tickets[row] = 0u;
+  lp_join(a, sh, row, sc, tok, z);
 }
 
 }  // namespace
@@ -365,15 +529,21 @@ hipError_t launch_token_logprobs(const ent_ctx* c, int T, const void* logits, in
   a.top_lp = top_logprobs;
   a.sums = c->lp_sums;
   a.keys = c->lp_keys;
+  a.tickets = c->lp_tickets;
   a.flags = c->dev_flags;
   const bool bf16 = logits_dtype == ENT_BF16;
-  const int tile = kLpThreads * (bf16 ? 8 : 4);          // logits of a workgroup's step
-  a.parts = std::max(1, std::min({kLpSlots / T, 64, (a.V + tile - 1) / tile}));
-  auto kern = bf16 ? logprobs_kernel<uint16_t> : logprobs_kernel<float>;
+  // Parts of a row.  A workgroup a CU, of 16 KB at least; where that leaves a part more
+  // than 32 KB, more of them, up to four a CU.  Us with 128 / 256 / 512 / 1024 workgroups
+  // (n_top 5, 128256 logits): 4 rows of floats 10.2 / 11.4, 16 rows 13.3 / 12.8 / 14.7,
+  // 64 rows - / 20.6 / 17.1 / 17.7, 64 of bf16 - / 17.2 / 17.1 / 18.8 (n_top 20: 18.1 /
+  // 15.7 / 17.9), 256 of bf16 - / 40 / 28 / 23.
+  const long long bytes = static_cast<long long>(a.V) * (bf16 ? 2 : 4);
+  const int part16 = static_cast<int>((bytes + 16383) / 16384);
+  a.parts = std::max(1, std::min({kLpParts, kLpSlots / T, std::max(std::min(c->num_cu / T, part16), (part16 + 1) / 2)}));
+  const bool stream = bytes * T > kLpStream;
+  auto kern = bf16 ? (stream ? logprobs_kernel<uint16_t, true> : logprobs_kernel<uint16_t, false>)
+                   : (stream ? logprobs_kernel<float, true> : logprobs_kernel<float, false>);
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(T) * a.parts), dim3(kLpThreads), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.parts == 1) return e;
-  hipLaunchKernelGGL(logprobs_join_kernel, dim3(T), dim3(64), 0, s, a, bf16 ? 1 : 0);
   return hipGetLastError();
 }
 
