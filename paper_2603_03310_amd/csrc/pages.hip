@@ -29,35 +29,60 @@ struct PageStore {
   int Hkv;
 };
 
-__device__ __forceinline__ void copy16(char* dst, const char* src, long long n, int t, int nt) {
-  const uint4* s = reinterpret_cast<const uint4*>(src);
-  uint4* d = reinterpret_cast<uint4*>(dst);
-  const int units = static_cast<int>(n / 16);
-  for (int i = t; i < units; i += 4 * nt) {
-    uint4 x[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i + u * nt < units) x[u] = s[i + u * nt];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i + u * nt < units) d[i + u * nt] = x[u];
-  }
+__device__ __forceinline__ const uint4* at16(const void* p, long long byte) {
+  return reinterpret_cast<const uint4*>(static_cast<const char*>(p) + byte);
+}
+__device__ __forceinline__ uint4* at16(void* p, long long byte) {
+  return reinterpret_cast<uint4*>(static_cast<char*>(p) + byte);
 }
 
-// Block `from`'s contents to block `to` by threads t of nt.
+// Block `from`'s contents to block `to` by threads t of nt: U pieces of keys and U of
+// values in flight a thread.
+template <int U>
 __device__ __forceinline__ void copy_block(const PageStore& st, int from, int to, int t, int nt) {
-  copy16(st.k + to * st.tile_bytes, st.k + from * st.tile_bytes, st.tile_bytes, t, nt);
-  copy16(st.v + to * st.tile_bytes, st.v + from * st.tile_bytes, st.tile_bytes, t, nt);
-  if (st.ksum)
-    copy16(reinterpret_cast<char*>(st.ksum + static_cast<long long>(to) * st.sum_floats),
-           reinterpret_cast<const char*>(st.ksum + static_cast<long long>(from) * st.sum_floats),
-           4ll * st.sum_floats, t, nt);
+  const uint4 *sk = at16(static_cast<const void*>(st.k), from * st.tile_bytes), *sv = at16(static_cast<const void*>(st.v), from * st.tile_bytes);
+  uint4 *dk = at16(st.k, to * st.tile_bytes), *dv = at16(st.v, to * st.tile_bytes);
+  const int units = static_cast<int>(st.tile_bytes / 16);
+  for (int i = t; i < units; i += U * nt) {
+    uint4 x[U], y[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * nt < units) {
+        x[u] = sk[i + u * nt];
+        y[u] = sv[i + u * nt];
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * nt < units) {
+        dk[i + u * nt] = x[u];
+        dv[i + u * nt] = y[u];
+      }
+  }
+  if (st.ksum) {
+    const uint4* s = at16(static_cast<const void*>(st.ksum), 4ll * from * st.sum_floats);
+    uint4* d = at16(st.ksum, 4ll * to * st.sum_floats);
+    for (int i = t; i < st.sum_floats / 4; i += nt) d[i] = s[i];
+  }
   if (st.ks) {
     for (int i = t; i < st.Hkv; i += nt) {
       st.ks[static_cast<long long>(to) * st.Hkv + i] = st.ks[static_cast<long long>(from) * st.Hkv + i];
       st.vs[static_cast<long long>(to) * st.Hkv + i] = st.vs[static_cast<long long>(from) * st.Hkv + i];
     }
   }
+}
+
+// Counting a launch's workgroups: the one whose count is the last does what has to wait
+// for all.  In two steps, each counter in a cache line of its own (a count on one line
+// takes about 10 ns); counters are 0 between launches.  One thread of each workgroup.
+constexpr int kCounters = 16;
+constexpr int kCounterPitch = 32;
+static_assert((kCounters + 1) * kCounterPitch <= kMinTickets, "counters");
+__device__ __forceinline__ bool count_out(unsigned* tickets) {
+  const unsigned n_wg = gridDim.x, c = blockIdx.x % kCounters;
+  const unsigned mine = (n_wg - c + kCounters - 1) / kCounters;      // workgroups of this counter
+  const unsigned used = n_wg < kCounters ? n_wg : kCounters;
+  if (mine > 1 && atomicInc(tickets + c * kCounterPitch, mine - 1) != mine - 1) return false;
+  return used == 1 || atomicInc(tickets + kCounters * kCounterPitch, used - 1) == used - 1;
 }
 
 // Sum of v over the threads before this one, and of all; the whole workgroup calls it.
@@ -86,9 +111,14 @@ struct Tables {
 };
 
 // ---------------------------------------------------------------------------
-// Fork.  One workgroup finds what each fork does: who is served, and its new
-// block from the free list; a second launch fills rows and copies blocks.
+// Fork.  Who is served, and with which new blocks, follows from all forks' rows and
+// lengths: up to kForkOne forks every workgroup finds it for itself (a fork a thread),
+// and the last to have done so moves the free list; more of them have one workgroup
+// find it in a launch of its own.  A fork's workgroups are of two sorts, those that fill
+// its row and count holders, and those that copy the begun block.
 // ---------------------------------------------------------------------------
+constexpr int kForkOne = kPageThreads;
+
 struct ForkArgs {
   Tables tb;
   int N;
@@ -99,62 +129,69 @@ struct ForkArgs {
   int n_ids;
   int* range;
   int4* rec;            // [N] (source row or -1, destination row, tokens, new block or -1)
+  unsigned* tickets;
+  int row_parts, parts; // workgroups of a fork that fill its row, and all of them
   PageStore st;
 };
 
-__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkArgs a) {
-  extern __shared__ int s_mem[];
-  __shared__ int s_red[kPlanThreads / 64];
+// What every fork does: emit(i, record).  Returns the free list's new lower end (its
+// old one where the range is bad).  mem: R + (R + 31) / 32 ints.
+template <int NT, typename F>
+__device__ __forceinline__ int fork_plan(const ForkArgs& a, int* mem, unsigned& bad, F emit) {
+  __shared__ int s_red[NT / 64];
   __shared__ int s_cut;
-  int* s_first = s_mem;                                          // [R] first fork to a row
-  unsigned* s_from = reinterpret_cast<unsigned*>(s_mem + a.tb.R);   // bits of rows that are forked
+  int* s_first = mem;                                            // [R] first fork to a row
+  unsigned* s_from = reinterpret_cast<unsigned*>(mem + a.tb.R);  // bits of rows that are forked
   const int t = threadIdx.x;
   const int head = a.range[0], end = a.range[1];
   const bool ring_ok = head >= 0 && head <= end && end <= a.n_ids;
   const int avail = ring_ok ? end - head : 0;
-  for (int i = t; i < a.tb.R; i += kPlanThreads) s_first[i] = 0x7fffffff;
-  for (int i = t; i < (a.tb.R + 31) / 32; i += kPlanThreads) s_from[i] = 0u;
+  for (int i = t; i < a.tb.R; i += NT) s_first[i] = 0x7fffffff;
+  for (int i = t; i < (a.tb.R + 31) / 32; i += NT) s_from[i] = 0u;
   if (t == 0) s_cut = ring_ok ? 0x7fffffff : 0;
   __syncthreads();
   auto row_ok = [&](int r) { return r >= 0 && r < a.tb.R; };
-  for (int i = t; i < a.N; i += kPlanThreads) {
-    const int s = a.src[i], d = a.dst[i];
-    if (row_ok(d)) atomicMin(&s_first[d], i);
-    if (row_ok(s)) atomicOr(&s_from[s / 32], 1u << (s % 32));
+  const int per = (a.N + NT - 1) / NT;       // consecutive forks of a thread
+  for (int k = 0; k < per; ++k) {
+    const int i = t * per + k;
+    if (i < a.N) {
+      const int s = a.src[i], d = a.dst[i];
+      if (row_ok(d)) atomicMin(&s_first[d], i);
+      if (row_ok(s)) atomicOr(&s_from[s / 32], 1u << (s % 32));
+    }
   }
   __syncthreads();
   // Fork i's tokens, or -1 where it is passed over.
-  unsigned bad = ring_ok ? 0u : ENT_DEV_BAD_TABLE;
+  bad |= ring_ok ? 0u : ENT_DEV_BAD_TABLE;
   auto tokens = [&](int i, int& s, int& d) {
     s = a.src[i];
     d = a.dst[i];
+    const int n = row_ok(s) ? a.tb.ctx[s] : 0;
     if (!row_ok(s) || !row_ok(d) || s_first[d] != i || (s_from[d / 32] >> (d % 32) & 1u)) {
       bad |= ENT_DEV_BAD_ROW;
       return -1;
     }
-    const int n = a.tb.ctx[s];
     if (n < 0 || n > a.tb.MAXB * kBlock) {
       bad |= ENT_DEV_BAD_CTXLEN;
       return -1;
     }
     return n;
   };
-  const int per = (a.N + kPlanThreads - 1) / kPlanThreads;
-  int need = 0, s, d;
+  int need = 0, s = 0, d = 0, n = -1;        // of the thread's last fork, its only one if per is 1
   for (int k = 0; k < per; ++k) {
     const int i = t * per + k;
     if (i < a.N) {
-      const int n = tokens(i, s, d);
+      n = tokens(i, s, d);
       need += n > 0 && n % kBlock != 0;
     }
   }
   int all;
-  const int before = scan_before<kPlanThreads>(need, all, s_red);
+  const int before = scan_before<NT>(need, all, s_red);
   need = before;
   for (int k = 0; k < per; ++k) {
     const int i = t * per + k;
     if (i < a.N) {
-      const int n = tokens(i, s, d);
+      if (per > 1) n = tokens(i, s, d);
       if (n > 0 && n % kBlock != 0 && ++need > avail) {
         atomicMin(&s_cut, i);
         break;
@@ -168,45 +205,67 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkArgs a) {
   for (int k = 0; k < per; ++k) {
     const int i = t * per + k;
     if (i < a.N) {
-      const int n = tokens(i, s, d);
-      const bool go = n >= 0 && i < cut;
-      int id = -1;
-      if (go && n % kBlock != 0) id = a.ids[head + need++];
-      a.rec[i] = make_int4(go ? s : -1, d, n, id);
+      if (per > 1) n = tokens(i, s, d);
+      const bool go = n >= 0 && i < cut, block = go && n % kBlock != 0;
+      emit(i, make_int4(go ? s : -1, d, n, block ? head + need : -1));
+      need += block;
     }
   }
-  // No fork reads a row that another writes.
-  __syncthreads();
-  for (int i = t; i < a.N; i += kPlanThreads) {
-    const int4 r = a.rec[i];
-    if (r.x >= 0) a.tb.ctx[r.y] = r.z;
-  }
-  if (t == 0 && ring_ok) a.range[0] = head + min(all, avail);
+  return ring_ok ? head + min(all, avail) : head;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkArgs a) {
+  extern __shared__ int s_mem[];
+  unsigned bad = 0;
+  const int head = fork_plan<kPlanThreads>(a, s_mem, bad, [&](int i, int4 r) { a.rec[i] = r; });
+  if (threadIdx.x == 0) a.range[0] = head;
   if (bad) raise_flag(a.tb.flags, bad);
 }
 
+// ONE: every workgroup plans for itself; else the records are there.
+template <bool ONE>
 __global__ __launch_bounds__(kPageThreads) void fork_kernel(ForkArgs a) {
-  const int4 r = a.rec[blockIdx.x];
-  if (r.x < 0) return;
-  const int t = blockIdx.y * kPageThreads + threadIdx.x, nt = gridDim.y * kPageThreads;
-  const int* from = a.tb.tables + static_cast<long long>(r.x) * a.tb.MAXB;
-  int* to = a.tb.tables + static_cast<long long>(r.y) * a.tb.MAXB;
-  const int full = r.z / kBlock;
+  extern __shared__ int s_mem[];
+  const int fork = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  int4 r;
+  int head = 0;
+  bool last = false;
   unsigned bad = 0;
-  for (int j = t; j < full; j += nt) {
-    const int p = from[j];
-    to[j] = p;
-    if (p >= 0 && p < a.tb.P) atomicAdd(&a.shared[p], 1);
-    else bad |= ENT_DEV_BAD_TABLE;
+  if constexpr (ONE) {
+    __shared__ int4 s_rec;
+    head = fork_plan<kPageThreads>(a, s_mem, bad, [&](int i, int4 x) { if (i == fork) s_rec = x; });
+    // Every workgroup finds the same; the first raises it.
+    if (blockIdx.x != 0) bad = 0;
+    __syncthreads();                        // the free list's range has been read
+    r = s_rec;
+    if (threadIdx.x == 0) last = count_out(a.tickets);
+  } else {
+    r = a.rec[fork];
   }
-  if (r.z % kBlock != 0) {
-    const int p = from[full];
-    const bool ok = r.w >= 0 && r.w < a.tb.P, there = p >= 0 && p < a.tb.P;
-    if (!ok || !there) bad |= ENT_DEV_BAD_TABLE;
-    if (t == 0) to[full] = ok ? r.w : -1;
-    if (ok && there) copy_block(a.st, p, r.w, t, nt);
+  if (r.x >= 0) {
+    const int* from = a.tb.tables + static_cast<long long>(r.x) * a.tb.MAXB;
+    int* to = a.tb.tables + static_cast<long long>(r.y) * a.tb.MAXB;
+    const int full = r.z / kBlock;
+    if (part < a.row_parts) {
+      for (int j = part * kPageThreads + threadIdx.x; j < full; j += a.row_parts * kPageThreads) {
+        const int p = from[j];
+        to[j] = p;
+        if (p >= 0 && p < a.tb.P) atomicAdd(&a.shared[p], 1);
+        else bad |= ENT_DEV_BAD_TABLE;
+      }
+      // No fork reads a row that another writes.
+      if (part == 0 && threadIdx.x == 0) a.tb.ctx[r.y] = r.z;
+    } else if (r.w >= 0) {
+      const int p = from[full], id = a.ids[r.w];
+      const bool ok = id >= 0 && id < a.tb.P, there = p >= 0 && p < a.tb.P;
+      const int t = (part - a.row_parts) * kPageThreads + threadIdx.x;
+      if (!ok || !there) bad |= ENT_DEV_BAD_TABLE;
+      if (t == 0) to[full] = ok ? id : -1;
+      if (ok && there) copy_block<2>(a.st, p, id, t, (a.parts - a.row_parts) * kPageThreads);
+    }
   }
   if (bad) raise_flag(a.tb.flags, bad);
+  if (last) a.range[0] = head;
 }
 
 // ---------------------------------------------------------------------------
@@ -403,7 +462,7 @@ __global__ __launch_bounds__(kPageThreads) void compact_kernel(CompactArgs a) {
   const long long me = static_cast<long long>(blockIdx.x) * kPageThreads + t;
   for (int m = blockIdx.x; m < moves; m += gridDim.x) {
     const int from = a.from[m], to = a.to[m];
-    copy_block(a.st, from, to, t, kPageThreads);
+    copy_block<4>(a.st, from, to, t, kPageThreads);
     if (a.shared && t == 0) {
       a.shared[to] = a.shared[from];
       a.shared[from] = 0;
@@ -458,12 +517,21 @@ hipError_t launch_cache_fork(const ent_ctx* c, int N, int R, const int* src, con
                              int* free_range, void* k_cache, void* v_cache, float* k_scale,
                              float* v_scale, float* ksum, hipStream_t s) {
   ForkArgs a{page_tables(c, R, tables, ctx_lens), N, src, dst, shared, free_ids, n_ids, free_range,
-             c->fork_rec, page_store(c, k_cache, v_cache, k_scale, v_scale, ksum)};
+             c->fork_rec, c->tickets, 1, 2, page_store(c, k_cache, v_cache, k_scale, v_scale, ksum)};
+  // Workgroups of a fork: of 256 to 1024 entries each for its row, of 8 KB at least for its
+  // block, about a thousand in all.
+  const int most = std::max(1, 512 / N);
+  a.row_parts = std::min(most, (c->cfg.max_blocks_per_seq + kPageThreads - 1) / kPageThreads);
+  a.parts = a.row_parts + static_cast<int>(std::min<long long>(most, (2 * a.st.tile_bytes + 8191) / 8192));
   const size_t lds = (static_cast<size_t>(R) + (R + 31) / 32) * sizeof(int);
+  if (N <= kForkOne) {
+    hipLaunchKernelGGL(fork_kernel<true>, dim3(N * a.parts), dim3(kPageThreads), lds, s, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), lds, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(fork_kernel, dim3(N, row_parts(c, N)), dim3(kPageThreads), 0, s, a);
+  hipLaunchKernelGGL(fork_kernel<false>, dim3(N * a.parts), dim3(kPageThreads), 0, s, a);
   return hipGetLastError();
 }
 
