@@ -284,13 +284,14 @@ int ent_init(const ent_config* cfg, ent_ctx** out) {
   const size_t sz_lpk = align_up(ent::kLpSlots * ENT_MAX_TOP_LOGPROBS * sizeof(unsigned long long));
   const size_t sz_lpt = align_up(ent::kLpSlots / 2 * sizeof(unsigned));
   const size_t sz_fork = align_up(Bm * sizeof(int4));
-  const size_t words = (static_cast<size_t>(f.num_pool_blocks) + 31) / 32;
-  const size_t sz_pbits = align_up(words * sizeof(unsigned));
-  const size_t sz_psums = align_up(words * sizeof(int2));
+  const size_t words = (static_cast<size_t>(f.num_pool_blocks) + 63) / 64;
+  const size_t sz_pbits = align_up(words * ent::kPageBitBytes);
+  const size_t sz_pwords = align_up(words * sizeof(unsigned long long));
+  const size_t sz_psums = align_up(words * sizeof(int));
   const size_t sz_pinfo = align_up(2 * sizeof(int));
   const size_t sz_flags = align_up(sizeof(unsigned));
   c->ws_bytes = sz_ent_part + sz_stats + sz_z + sz_lse + sz_lrow + sz_isc + sz_kphys + sz_acc + sz_ml +
-                sz_rec + sz_tmax + sz_ex + sz_tick + sz_lps + sz_lpk + sz_lpt + sz_fork + sz_pbits + sz_psums +
+                sz_rec + sz_tmax + sz_ex + sz_tick + sz_lps + sz_lpk + sz_lpt + sz_fork + sz_pbits + sz_pwords + sz_psums +
                 sz_pinfo + sz_flags;
   e = hipMalloc(&c->ws, c->ws_bytes);
   if (e != hipSuccess) {
@@ -325,8 +326,9 @@ int ent_init(const ent_config* cfg, ent_ctx** out) {
   c->lp_keys = reinterpret_cast<unsigned long long*>(take(sz_lpk));
   c->lp_tickets = reinterpret_cast<unsigned*>(take(sz_lpt));
   c->fork_rec = reinterpret_cast<int4*>(take(sz_fork));
-  c->page_bits = reinterpret_cast<unsigned*>(take(sz_pbits));
-  c->page_sums = reinterpret_cast<int2*>(take(sz_psums));
+  c->page_bits = reinterpret_cast<unsigned long long*>(take(sz_pbits));
+  c->page_words = reinterpret_cast<unsigned long long*>(take(sz_pwords));
+  c->page_sums = reinterpret_cast<int*>(take(sz_psums));
   c->page_info = reinterpret_cast<int*>(take(sz_pinfo));
   c->dev_flags = reinterpret_cast<unsigned*>(take(sz_flags));
   *out = c;

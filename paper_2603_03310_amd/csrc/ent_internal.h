@@ -17,6 +17,7 @@ constexpr int kMaxGroup = 16;               // query heads per KV head
 constexpr int kMinTickets = 1024;           // counters in the workspace, at least
 constexpr int kMaxBlocksPerSeq = 16384;     // selection keeps all scores in LDS
 constexpr int kEstChunkThreads = 256;       // threads of an entropy chunk job (maxima per chunk)
+constexpr int kPageBitBytes = 64;           // from one word of the block bitmap to the next
 constexpr int kLpSlots = 1024;              // parts of the rows that log probabilities are cut into
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -88,8 +89,10 @@ struct ent_ctx {
   unsigned* lp_tickets = nullptr; // [kLpSlots / 2]  finished parts of rows (zero between launches)
   unsigned long long* lp_keys = nullptr;   // [kLpSlots, ENT_MAX_TOP_LOGPROBS]  their largest logits
   int4* fork_rec = nullptr;       // [max_batch]  what each fork does
-  unsigned* page_bits = nullptr;  // [(P + 31) / 32]  a set of blocks (zero between calls)
-  int2* page_sums = nullptr;      // [(P + 31) / 32]  the set again, with its prefix sums
+  unsigned long long* page_bits = nullptr;   // a word per 64 blocks, kPageBitBytes apart: a set of
+                                             // blocks (zero between calls)
+  unsigned long long* page_words = nullptr;  // [(P + 63) / 64]  the set again, side by side
+  int* page_sums = nullptr;       // [(P + 63) / 64]  blocks of the set before each word
   int* page_info = nullptr;       // [2]  numbers of used blocks (compact)
   unsigned* dev_flags = nullptr;  // [1]
 

@@ -5,17 +5,24 @@
 // every full block of its parent and copies the last, begun one, if any; a release
 // takes one from every block of its sequences, and those that had none left over are
 // free.  Sets of blocks are bitmaps of the pool, so what comes out of them is in
-// ascending order whatever order the atomics came in.
+// ascending order whatever order the atomics came in.  Their words lie 64 bytes apart:
+// atomics on one cache line come one after the other, and side by side a line would
+// hold 1024 blocks.
 
 #include "ent_internal.h"
 
 #include <algorithm>
 
+#ifndef KDENSE
+#define KDENSE 8
+#endif
 namespace ent {
 namespace {
 
 constexpr int kPageThreads = 256;
 constexpr int kPlanThreads = 1024;
+constexpr int kDense = KDENSE;          // bits of a word, on average, that a wave writes together
+constexpr int kBitPitch = kPageBitBytes / 8;     // 64-bit words from one word of a bitmap to the next
 
 // Where a block's contents lie: caches of tile_bytes a block, mean keys, scales.
 struct PageStore {
@@ -34,6 +41,20 @@ __device__ __forceinline__ const uint4* at16(const void* p, long long byte) {
 }
 __device__ __forceinline__ uint4* at16(void* p, long long byte) {
   return reinterpret_cast<uint4*>(static_cast<char*>(p) + byte);
+}
+
+template <int U>
+__device__ __forceinline__ void copy_units(const uint4* __restrict__ s, uint4* __restrict__ d, int units, int t,
+                                           int nt) {
+  int i = t;
+  for (; i + (U - 1) * nt < units; i += U * nt) {
+    uint4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = s[i + u * nt];
+#pragma unroll
+    for (int u = 0; u < U; ++u) d[i + u * nt] = x[u];
+  }
+  for (; i < units; i += nt) d[i] = s[i];
 }
 
 // Block `from`'s contents to block `to` by threads t of nt: U pieces of keys and U of
@@ -58,11 +79,9 @@ __device__ __forceinline__ void copy_block(const PageStore& st, int from, int to
         dv[i + u * nt] = y[u];
       }
   }
-  if (st.ksum) {
-    const uint4* s = at16(static_cast<const void*>(st.ksum), 4ll * from * st.sum_floats);
-    uint4* d = at16(st.ksum, 4ll * to * st.sum_floats);
-    for (int i = t; i < st.sum_floats / 4; i += nt) d[i] = s[i];
-  }
+  if (st.ksum)
+    copy_units<1>(at16(static_cast<const void*>(st.ksum), 4ll * from * st.sum_floats),
+                  at16(st.ksum, 4ll * to * st.sum_floats), st.sum_floats / 4, t, nt);
   if (st.ks) {
     for (int i = t; i < st.Hkv; i += nt) {
       st.ks[static_cast<long long>(to) * st.Hkv + i] = st.ks[static_cast<long long>(from) * st.Hkv + i];
@@ -101,6 +120,74 @@ __device__ __forceinline__ int scan_before(int v, int& all, int* red) {
   }
   __syncthreads();
   return out;
+}
+
+// Bitmaps of blocks: a 64-bit word per 64 of them.
+typedef unsigned long long u64;
+__device__ __forceinline__ int popc(u64 b) { return static_cast<int>(__popcll(b)); }
+__device__ __forceinline__ bool set_bit(u64* bits, int p) {
+  const u64 bit = 1ull << (p % 64);
+  return (atomicOr(&bits[static_cast<long long>(p / 64) * kBitPitch], bit) & bit) != 0;
+}
+__device__ __forceinline__ u64 look_word(const u64* bits, int w, int words) {
+  return w < words ? __hip_atomic_load(bits + static_cast<long long>(w) * kBitPitch, __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT)
+                   : 0ull;
+}
+// ... and cleared for the next call.
+__device__ __forceinline__ u64 take_word(u64* bits, int w, int words) {
+  const u64 b = look_word(bits, w, words);
+  if (b) bits[static_cast<long long>(w) * kBitPitch] = 0ull;
+  return b;
+}
+// The bits of b below this lane's, and this lane's (b the same in every lane).
+__device__ __forceinline__ int bits_below(u64 b) {
+  return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(b >> 32),
+                                                    __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(b), 0u)));
+}
+__device__ __forceinline__ bool bit_here(u64 b) { return (b >> (threadIdx.x & 63) & 1ull) != 0; }
+// A workgroup's words (word t of thread t, `n` of them), each with a value: f(word, value,
+// t) by all lanes of a wave, lane l for bit l, with consecutive words dealt to the waves and
+// four of them together (one after the other, a word is a chain of some 25 instructions:
+// 120 ns).  s_b, s_v: a place per thread.
+template <int NT, typename F>
+__device__ __forceinline__ void each_word(u64 b, int v, int n, u64* s_b, int* s_v, F f) {
+  constexpr int W = NT / 64, Q = 4;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  s_b[t] = b;
+  s_v[t] = v;
+  __syncthreads();
+  const u64 mb = s_b[lane * W + wave];
+  const int mv = s_v[lane * W + wave];
+  for (int i = 0; i < 64 && i * W + wave < n; i += Q) {
+    u64 w[Q], any = 0ull;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      w[q] = static_cast<u64>(static_cast<unsigned>(lane_at(static_cast<int>(mb >> 32), i + q))) << 32 |
+             static_cast<unsigned>(lane_at(static_cast<int>(mb), i + q));
+      any |= w[q];
+    }
+    if (any == 0ull) continue;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) f(w[q], lane_at(mv, i + q), (i + q) * W + wave);
+  }
+  __syncthreads();
+}
+
+// Writes the ids of a workgroup's words (word t of thread t, of ids from id0 on; at most n
+// words with bits), the first of a thread's at `at` and so on; those before place 0 are
+// left out.  Where a word has few bits, each thread writes its own.
+template <int NT>
+__device__ __forceinline__ void list_bits(u64 b, int at, int id0, int n, bool dense, int* out, u64* s_b, int* s_v) {
+  if (dense) {
+    each_word<NT>(b, at, n, s_b, s_v, [&](u64 w, int first, int i) {
+      const int place = first + bits_below(w);
+      if (bit_here(w) && place >= 0) out[place] = id0 + i * 64 + static_cast<int>(threadIdx.x & 63);
+    });
+  } else {
+    for (; b; b &= b - 1, ++at)
+      if (at >= 0) out[at] = id0 + static_cast<int>(threadIdx.x) * 64 + __builtin_ctzll(b);
+  }
 }
 
 struct Tables {
@@ -269,8 +356,10 @@ __global__ __launch_bounds__(kPageThreads) void fork_kernel(ForkArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Release.  A first launch takes a holder from every block and marks those that
-// had none left; one workgroup then lists the marked ones.
+// Release.  Every workgroup takes a holder from some of its sequence's blocks; a block
+// that had none left over keeps its count of 0 and goes into a bitmap.  The last
+// workgroup lists the bitmap, 64 blocks a wave and step, and clears it.  Bound by the
+// chain of round trips (row, length, entry, count, bit, workgroup count, bitmap).
 // ---------------------------------------------------------------------------
 struct ReleaseArgs {
   Tables tb;
@@ -280,90 +369,69 @@ struct ReleaseArgs {
   int* ids;
   int n_ids;
   int* range;
-  unsigned* bits;       // [(P + 31) / 32], zero between calls
+  u64* bits;            // a word per 64 blocks, kBitPitch apart, zero between calls
+  unsigned* tickets;
+  int parts;            // workgroups of a sequence
 };
 
-__device__ __forceinline__ bool range_ok(const int* range, int n_ids, int& head) {
-  head = range[0];
-  const int end = range[1];
-  return head >= 0 && head <= end && end <= n_ids;
-}
-
-__global__ __launch_bounds__(kPageThreads) void release_kernel(ReleaseArgs a) {
-  const int i = blockIdx.x;
-  const bool first = blockIdx.y == 0 && threadIdx.x == 0;
-  int head;
-  if (!range_ok(a.range, a.n_ids, head)) {
-    if (first && i == 0) raise_flag(a.tb.flags, ENT_DEV_BAD_TABLE);
+__global__ __launch_bounds__(kPlanThreads) void release_kernel(ReleaseArgs a) {
+  __shared__ u64 s_b[kPlanThreads];
+  __shared__ int s_v[kPlanThreads], s_red[kPlanThreads / 64];
+  __shared__ int s_last;
+  constexpr int NT = kPlanThreads;
+  const int t = threadIdx.x, i = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  const int row = a.rows[i], head = a.range[0], end = a.range[1];
+  if (head < 0 || head > end || end > a.n_ids) {       // for every workgroup: none is counted
+    if (blockIdx.x == 0 && t == 0) raise_flag(a.tb.flags, ENT_DEV_BAD_TABLE);
     return;
   }
-  const int row = a.rows[i];
-  bool twice = false;
-  for (int k = threadIdx.x; k < i; k += kPageThreads) twice |= a.rows[k] == row;
-  if (__syncthreads_or(twice) || row < 0 || row >= a.tb.R) {
-    if (first) raise_flag(a.tb.flags, ENT_DEV_BAD_ROW);
-    return;
-  }
-  const int n = a.tb.ctx[row];
-  if (n < 0 || n > a.tb.MAXB * kBlock) {
-    if (first) raise_flag(a.tb.flags, ENT_DEV_BAD_CTXLEN);
-    return;
-  }
-  const int nb = (n + kBlock - 1) / kBlock;
-  const int* tab = a.tb.tables + static_cast<long long>(row) * a.tb.MAXB;
   unsigned bad = 0;
-  for (int j = blockIdx.y * kPageThreads + threadIdx.x; j < nb; j += gridDim.y * kPageThreads) {
-    const int p = tab[j];
-    if (p < 0 || p >= a.tb.P) {
-      bad |= ENT_DEV_BAD_TABLE;
-      continue;
-    }
-    const unsigned bit = 1u << (p % 32);
-    if (a.shared) {
-      const int old = atomicSub(&a.shared[p], 1);
-      if (old <= 0) atomicOr(&a.bits[p / 32], bit);
-      if (old < 0) bad |= ENT_DEV_BAD_TABLE;
-    } else if (atomicOr(&a.bits[p / 32], bit) & bit) {
-      bad |= ENT_DEV_BAD_TABLE;
+  auto length = [&](int r) { return r >= 0 && r < a.tb.R ? a.tb.ctx[r] : -1; };
+  auto length_ok = [&](int n) { return n >= 0 && n <= a.tb.MAXB * kBlock; };
+  const int n = length(row);
+  bool twice = false;
+  for (int k = t; k < i; k += NT) twice |= a.rows[k] == row;
+  if (__syncthreads_or(twice) || row < 0 || row >= a.tb.R) {
+    bad = ENT_DEV_BAD_ROW;
+  } else if (!length_ok(n)) {
+    bad = ENT_DEV_BAD_CTXLEN;
+  } else {
+    const int nb = (n + kBlock - 1) / kBlock;
+    const int* tab = a.tb.tables + static_cast<long long>(row) * a.tb.MAXB;
+    // Whoever finds no holder left gives the count back, so it ends at 0; who finds the
+    // bit set then is one too many.
+    for (int j = part * NT + t; j < nb; j += a.parts * NT) {
+      const int p = tab[j];
+      if (p < 0 || p >= a.tb.P) {
+        bad |= ENT_DEV_BAD_TABLE;
+      } else if (!a.shared || atomicSub(&a.shared[p], 1) <= 0) {
+        if (a.shared) atomicAdd(&a.shared[p], 1);
+        if (set_bit(a.bits, p)) bad |= ENT_DEV_BAD_TABLE;
+      }
     }
   }
   if (bad) raise_flag(a.tb.flags, bad);
-}
+  __builtin_amdgcn_s_waitcnt(0);            // this wave's bits are set
+  __syncthreads();
+  if (t == 0) s_last = count_out(a.tickets);
+  __syncthreads();
+  if (!s_last) return;
 
-__global__ __launch_bounds__(kPlanThreads) void release_list_kernel(ReleaseArgs a) {
-  __shared__ int s_red[kPlanThreads / 64];
-  const int t = threadIdx.x;
-  int head;
-  if (!range_ok(a.range, a.n_ids, head)) return;
-  const int words = (a.tb.P + 31) / 32;
-  int total = 0, all;
-  for (int w0 = 0; w0 < words; w0 += kPlanThreads) {
-    int n = 0;
-    if (w0 + t < words) n = __popc(a.bits[w0 + t]);
-    (void)scan_before<kPlanThreads>(n, all, s_red);
-    total += all;
+  const int words = (a.tb.P + 63) / 64;
+  u64 x = take_word(a.bits, t, words);
+  for (int k = t; k < a.N; k += NT) {
+    const int r = a.rows[k];
+    if (length_ok(length(r))) a.tb.ctx[r] = 0;
   }
-  int at = head - total;                 // place of the first; those below 0 find no room
-  for (int w0 = 0; w0 < words; w0 += kPlanThreads) {
-    unsigned b = 0;
-    if (w0 + t < words) b = a.bits[w0 + t];
-    int k = at + scan_before<kPlanThreads>(__popc(b), all, s_red);
-    if (b) a.bits[w0 + t] = 0u;
-    while (b) {
-      const int p = (w0 + t) * 32 + __builtin_ctz(b);
-      b &= b - 1;
-      if (k >= 0) a.ids[k] = p;
-      ++k;
-      if (a.shared) a.shared[p] = 0;
-    }
-    at += all;
-  }
-  for (int i = t; i < a.N; i += kPlanThreads) {
-    const int row = a.rows[i];
-    if (row >= 0 && row < a.tb.R) {
-      const int n = a.tb.ctx[row];
-      if (n >= 0 && n <= a.tb.MAXB * kBlock) a.tb.ctx[row] = 0;
-    }
+  int total = popc(x), all;
+  for (int w = NT + t; w < words; w += NT) total += popc(look_word(a.bits, w, words));
+  int k = scan_before<NT>(total, total, s_red);
+  int at = head - total;                    // place of the first; those below 0 find no room
+  for (int w0 = 0; w0 < words; w0 += NT) {
+    if (w0 > 0) x = take_word(a.bits, w0 + t, words);
+    if (words > NT) k = scan_before<NT>(popc(x), all, s_red);
+    list_bits<NT>(x, at + k, w0 * 64, words - w0, total >= kDense * words, a.ids, s_b, s_v);
+    if (words > NT) at += all;
   }
   if (t == 0) {
     a.range[0] = max(head - total, 0);
@@ -372,10 +440,11 @@ __global__ __launch_bounds__(kPlanThreads) void release_list_kernel(ReleaseArgs 
 }
 
 // ---------------------------------------------------------------------------
-// Compact.  Blocks in use as a bitmap; one workgroup forms its prefix sums, their
-// number U, and who moves where (the i-th used block from U on to the i-th free
-// place below U); then contents, counts, tables and the free list.  Places that are
-// written (below U, free) and read (from U on) do not meet, so moves are in any order.
+// Compact.  Blocks in use as a bitmap; the last workgroup to mark some forms its prefix
+// sums, their number U, and who moves where (the i-th used block from U on to the i-th
+// free place below U).  A second launch moves contents and counts, and rewrites tables
+// and the free list.  Places that are written (below U, free) and read (from U on) do not
+// meet, so moves are in any order.
 // ---------------------------------------------------------------------------
 struct CompactArgs {
   Tables tb;
@@ -384,67 +453,78 @@ struct CompactArgs {
   int n_ids;
   int* range;
   int* n_used;          // nullable
-  unsigned* bits;
-  int2* sums;           // [(P + 31) / 32] (used blocks before the word, the word)
+  u64* bits;
+  u64* words;           // [(P + 63) / 64]  the bitmap again
+  int* sums;            // [(P + 63) / 64]  used blocks before the word
   int* from;            // [used] moves
   int* to;
   int* info;            // U, used blocks below U
+  unsigned* tickets;
+  int parts;            // workgroups of a row of the tables
+  int row_wgs;          // of all rows
   PageStore st;
 };
 
-__global__ __launch_bounds__(kPageThreads) void mark_kernel(CompactArgs a) {
-  const int row = blockIdx.x;
+__global__ __launch_bounds__(kPlanThreads) void mark_kernel(CompactArgs a) {
+  __shared__ u64 s_b[kPlanThreads];
+  __shared__ int s_v[kPlanThreads], s_red[kPlanThreads / 64];
+  __shared__ int s_below, s_last;
+  constexpr int NT = kPlanThreads;
+  const int t = threadIdx.x, row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
   const int n = a.tb.ctx[row];
+  unsigned bad = 0;
   if (n < 0 || n > a.tb.MAXB * kBlock) {
-    if (blockIdx.y == 0 && threadIdx.x == 0) raise_flag(a.tb.flags, ENT_DEV_BAD_CTXLEN);
-    return;
+    bad = ENT_DEV_BAD_CTXLEN;
+  } else {
+    const int nb = (n + kBlock - 1) / kBlock;
+    const int* tab = a.tb.tables + static_cast<long long>(row) * a.tb.MAXB;
+    for (int j = part * NT + t; j < nb; j += a.parts * NT) {
+      const int p = tab[j];
+      if (p >= 0 && p < a.tb.P) set_bit(a.bits, p);
+      else bad |= ENT_DEV_BAD_TABLE;
+    }
   }
-  const int nb = (n + kBlock - 1) / kBlock;
-  const int* tab = a.tb.tables + static_cast<long long>(row) * a.tb.MAXB;
-  bool bad = false;
-  for (int j = blockIdx.y * kPageThreads + threadIdx.x; j < nb; j += gridDim.y * kPageThreads) {
-    const int p = tab[j];
-    if (p >= 0 && p < a.tb.P) atomicOr(&a.bits[p / 32], 1u << (p % 32));
-    else bad = true;
-  }
-  if (bad) raise_flag(a.tb.flags, ENT_DEV_BAD_TABLE);
-}
+  if (bad) raise_flag(a.tb.flags, bad);
+  __builtin_amdgcn_s_waitcnt(0);            // this wave's bits are set
+  __syncthreads();
+  if (t == 0) s_last = count_out(a.tickets);
+  __syncthreads();
+  if (!s_last) return;
 
-__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactArgs a) {
-  __shared__ int s_red[kPlanThreads / 64];
-  __shared__ int s_below;
-  const int t = threadIdx.x;
-  const int words = (a.tb.P + 31) / 32;
-  int U = 0, all;
-  for (int w0 = 0; w0 < words; w0 += kPlanThreads) {
-    unsigned b = 0;
-    if (w0 + t < words) b = a.bits[w0 + t];
-    const int k = U + scan_before<kPlanThreads>(__popc(b), all, s_red);
-    if (w0 + t < words) {
-      a.sums[w0 + t] = make_int2(k, static_cast<int>(b));
-      a.bits[w0 + t] = 0u;
+  const int words = (a.tb.P + 63) / 64;
+  int U = 0, k = 0, all;
+  u64 x = 0;
+  for (int w0 = 0; w0 < words; w0 += NT) {
+    const int w = w0 + t;
+    x = take_word(a.bits, w, words);
+    k = U + scan_before<NT>(popc(x), all, s_red);
+    if (w < words) {
+      a.words[w] = x;
+      a.sums[w] = k;
     }
     U += all;
   }
-  if (t == 0) s_below = U;               // where U is the whole pool
+  // A thread meets its own words again (in registers where there is one step).
+  if (t == 0) s_below = U;                  // where U is the whole pool, in whole words
   __syncthreads();
-  // Each thread reads back what it wrote itself.
-  for (int w = t; w < words; w += kPlanThreads) {
-    const int2 v = a.sums[w];
-    if (w == U / 32) s_below = v.x + __popc(static_cast<unsigned>(v.y) & ((1u << (U % 32)) - 1u));
+  const int last = U / 64;                  // the word that U lies in
+  if (last < words && last % NT == t) {
+    const bool here = words <= NT;
+    s_below = (here ? k : a.sums[last]) + popc((here ? x : a.words[last]) & ((1ull << (U % 64)) - 1ull));
   }
   __syncthreads();
   const int below = s_below;
-  for (int w = t; w < words; w += kPlanThreads) {
-    const int2 v = a.sums[w];
-    const int base = w * 32;
-    unsigned used = static_cast<unsigned>(v.y), free = ~used;
+  for (int w0 = 0; w0 < words; w0 += NT) {
+    const int w = w0 + t, base = w * 64;
+    if (words > NT) {
+      x = w < words ? a.words[w] : 0ull;
+      k = w < words ? a.sums[w] : 0;
+    }
     // Bits of ids below U.
-    const unsigned low = base + 32 <= U ? ~0u : base >= U ? 0u : (1u << (U - base)) - 1u;
-    int hole = base - v.x;               // free ids before the word
-    for (unsigned m = free & low; m; m &= m - 1) a.to[hole++] = base + __builtin_ctz(m);
-    int k = v.x + __popc(used & low) - below;
-    for (unsigned m = used & ~low; m; m &= m - 1) a.from[k++] = base + __builtin_ctz(m);
+    const u64 low = w >= words || base >= U ? 0ull : base + 64 <= U ? ~0ull : (1ull << (U - base)) - 1ull;
+    const bool dense = U - below >= kDense * words;
+    list_bits<NT>(~x & low, base - k, w0 * 64, words - w0, dense, a.to, s_b, s_v);
+    list_bits<NT>(x & ~low, k + popc(x & low) - below, w0 * 64, words - w0, dense, a.from, s_b, s_v);
   }
   if (t == 0) {
     a.info[0] = U;
@@ -455,34 +535,47 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactArgs 
   }
 }
 
+// Workgroups [0, row_wgs) take rows of the tables and the free list, the others blocks:
+// one the keys and what belongs to them, one the values.
 __global__ __launch_bounds__(kPageThreads) void compact_kernel(CompactArgs a) {
   const int U = a.info[0], below = a.info[1], moves = U - below;
   const int t = threadIdx.x;
-  const long long all = static_cast<long long>(gridDim.x) * kPageThreads;
-  const long long me = static_cast<long long>(blockIdx.x) * kPageThreads + t;
-  for (int m = blockIdx.x; m < moves; m += gridDim.x) {
-    const int from = a.from[m], to = a.to[m];
-    copy_block<4>(a.st, from, to, t, kPageThreads);
-    if (a.shared && t == 0) {
-      a.shared[to] = a.shared[from];
-      a.shared[from] = 0;
+  if (blockIdx.x >= static_cast<unsigned>(a.row_wgs)) {
+    const int units = static_cast<int>(a.st.tile_bytes / 16);
+    for (int m = blockIdx.x - a.row_wgs; m < 2 * moves; m += gridDim.x - a.row_wgs) {
+      const int from = a.from[m >> 1], to = a.to[m >> 1];
+      const bool keys = (m & 1) == 0;
+      char* const base = keys ? a.st.k : a.st.v;
+      copy_units<8>(at16(static_cast<const void*>(base), from * a.st.tile_bytes), at16(base, to * a.st.tile_bytes),
+                    units, t, kPageThreads);
+      if (keys && a.st.ksum)
+        copy_units<1>(at16(static_cast<const void*>(a.st.ksum), 4ll * from * a.st.sum_floats),
+                      at16(a.st.ksum, 4ll * to * a.st.sum_floats), a.st.sum_floats / 4, t, kPageThreads);
+      if (a.st.ks) {
+        float* sc = keys ? a.st.ks : a.st.vs;
+        for (int i = t; i < a.st.Hkv; i += kPageThreads)
+          sc[static_cast<long long>(to) * a.st.Hkv + i] = sc[static_cast<long long>(from) * a.st.Hkv + i];
+      }
+      if (!keys && a.shared && t == 0) {
+        a.shared[to] = a.shared[from];
+        a.shared[from] = 0;
+      }
     }
-  }
-  // Tables: entries from U on follow their blocks.
-  if (moves > 0) {
-    const long long entries = static_cast<long long>(a.tb.R) * a.tb.MAXB;
-    for (long long e = me; e < entries; e += all) {
-      const int row = static_cast<int>(e / a.tb.MAXB), j = static_cast<int>(e % a.tb.MAXB);
-      const int n = a.tb.ctx[row];
-      if (n < 0 || n > a.tb.MAXB * kBlock || j >= (n + kBlock - 1) / kBlock) continue;
-      const int p = a.tb.tables[e];
-      if (p < U || p >= a.tb.P) continue;
-      const int2 v = a.sums[p / 32];
-      a.tb.tables[e] = a.to[v.x + __popc(static_cast<unsigned>(v.y) & ((1u << (p % 32)) - 1u)) - below];
-    }
+    return;
   }
   const int first = a.n_ids - (a.tb.P - U);
-  for (long long i = me; i < a.tb.P - U; i += all) a.ids[first + i] = U + static_cast<int>(i);
+  for (int i = blockIdx.x * kPageThreads + t; i < a.tb.P - U; i += a.row_wgs * kPageThreads) a.ids[first + i] = U + i;
+  if (moves == 0) return;
+  const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  const int n = a.tb.ctx[row];
+  if (n < 0 || n > a.tb.MAXB * kBlock) return;
+  const int nb = (n + kBlock - 1) / kBlock;
+  int* tab = a.tb.tables + static_cast<long long>(row) * a.tb.MAXB;
+  for (int j = part * kPageThreads + t; j < nb; j += a.parts * kPageThreads) {
+    const int p = tab[j];
+    if (p < U || p >= a.tb.P) continue;
+    tab[j] = a.to[a.sums[p / 64] + popc(a.words[p / 64] & ((1ull << (p % 64)) - 1ull)) - below];
+  }
 }
 
 PageStore page_store(const ent_ctx* c, void* k, void* v, float* ks, float* vs, float* ksum) {
@@ -504,10 +597,9 @@ Tables page_tables(const ent_ctx* c, int R, const int* tables, int* ctx) {
   return Tables{const_cast<int*>(tables), ctx, R, c->cfg.max_blocks_per_seq, c->cfg.num_pool_blocks, c->dev_flags};
 }
 
-// Workgroups that share a row's entries: about a thousand in all, 256 entries each at least.
-unsigned row_parts(const ent_ctx* c, int rows) {
-  const int most = (c->cfg.max_blocks_per_seq + kPageThreads - 1) / kPageThreads;
-  return static_cast<unsigned>(std::max(1, std::min(most, 1024 / std::max(rows, 1))));
+// Workgroups of NT threads that share a row's entries: about a thousand in all.
+int row_parts(const ent_ctx* c, int rows, int nt) {
+  return std::max(1, std::min(1024 / rows, (c->cfg.max_blocks_per_seq + nt - 1) / nt));
 }
 
 }  // namespace
@@ -539,11 +631,8 @@ hipError_t launch_cache_release(const ent_ctx* c, int N, int R, const int* rows,
                                 int* ctx_lens, int* shared, int* free_ids, int n_ids,
                                 int* free_range, hipStream_t s) {
   ReleaseArgs a{page_tables(c, R, tables, ctx_lens), N, rows, shared, free_ids, n_ids, free_range,
-                c->page_bits};
-  hipLaunchKernelGGL(release_kernel, dim3(N, row_parts(c, N)), dim3(kPageThreads), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(release_list_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+                c->page_bits, c->tickets, row_parts(c, N, kPlanThreads)};
+  hipLaunchKernelGGL(release_kernel, dim3(N * a.parts), dim3(kPlanThreads), 0, s, a);
   return hipGetLastError();
 }
 
@@ -552,15 +641,15 @@ hipError_t launch_cache_compact(const ent_ctx* c, int R, int* tables, const int*
                                 void* v_cache, float* k_scale, float* v_scale, float* ksum,
                                 int* n_used, hipStream_t s) {
   CompactArgs a{page_tables(c, R, tables, const_cast<int*>(ctx_lens)), shared, free_ids, n_ids, free_range,
-                n_used, c->page_bits, c->page_sums, c->kept_phys, reinterpret_cast<int*>(c->iscores),
-                c->page_info, page_store(c, k_cache, v_cache, k_scale, v_scale, ksum)};
-  hipLaunchKernelGGL(mark_kernel, dim3(R, row_parts(c, R)), dim3(kPageThreads), 0, s, a);
-  hipError_t e = hipGetLastError();
+                n_used, c->page_bits, c->page_words, c->page_sums, c->kept_phys,
+                reinterpret_cast<int*>(c->iscores), c->page_info, c->tickets,
+                row_parts(c, R, kPlanThreads), 0, page_store(c, k_cache, v_cache, k_scale, v_scale, ksum)};
+  hipLaunchKernelGGL(mark_kernel, dim3(R * a.parts), dim3(kPlanThreads), 0, s, a);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(compact_kernel, dim3(4 * c->num_cu), dim3(kPageThreads), 0, s, a);
+  a.parts = row_parts(c, R, kPageThreads);
+  a.row_wgs = R * a.parts;
+  hipLaunchKernelGGL(compact_kernel, dim3(a.row_wgs + 8 * c->num_cu), dim3(kPageThreads), 0, s, a);
   return hipGetLastError();
 }
 
