@@ -39,9 +39,9 @@ constexpr int kLpSegs = 8;            // segments of a thread's walk
 static_assert(kLpTop * kLpTop <= kLpCand, "keys of a row's n lists");
 static_assert(kLpTop + kLpTop / 2 + 3 <= kLpWho, "threads over the bound");
 static_assert(kLpParts == 64 && kLpParts <= kLpThreads, "a wave joins the parts");
-constexpr int kLpUnroll = 4;          // pieces of a thread in flight
 // Logits past what the last-level cache holds are read without a place in the caches:
-// 2500 rows of 128256 floats 238 us against 257 with; 64 rows of bf16 18.8 against 18.4.
+// 2500 rows of 128256 floats 238 us against 257 with (then with 8 pieces of a thread in
+// flight 212, with 4 217); 64 rows of bf16 18.8 against 18.4.
 constexpr long long kLpStream = 256ll << 20;
 typedef unsigned long long u64;
 
@@ -163,9 +163,11 @@ __device__ __forceinline__ V lp_shared(const V* p) {
 
 struct LpShared {
   u64 key[kLpThreads];       // per thread: its largest logit (of its maxima, first piece)
-  u64 cand[kLpCand];
+  union {
+    float seg[kLpSegs][kLpThreads]; // ... in each segment, until `again` is made of it
+    u64 cand[kLpCand];
+  };
   float red[3 * kLpThreads / 64];
-  float seg[kLpSegs][kLpThreads];   // ... in each segment
   int again[kLpWho * kLpSegs];      // (segment, thread) that are read again
   u64 edge;
   int count, agains, last;
@@ -397,7 +399,8 @@ __device__ __forceinline__ void lp_join(const LpArgs& a, LpShared& sh, int row, 
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs a) {
   using R = Row<T, STREAM>;
-  constexpr int N = R::N, NT = kLpThreads, U = kLpUnroll;
+  constexpr int N = R::N, NT = kLpThreads;
+  constexpr int U = STREAM ? 8 : 4;        // pieces of a thread in flight
   __shared__ LpShared sh;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;

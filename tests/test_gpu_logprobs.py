@@ -58,7 +58,7 @@ def check(z, got, tokens, n_top, temp=None, t_cal=1.0):
         assert abs(h[t] - r[1]) <= b[1], (t, h[t], r[1])
         fin = np.isfinite(r[3])
         assert np.array_equal(top[t][~fin], r[3][~fin].astype(np.float32))
-        assert (np.abs(top[t] - r[3])[fin] <= b[0][fin]).all()
+        assert (np.abs(top[t][fin] - r[3][fin]) <= b[0][fin]).all()
         if tokens is not None:
             if tok >= V:
                 assert np.isnan(lp[t])
