@@ -125,9 +125,8 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
   const int half = a.rot / 2;
   const bool turns = PAIRS == kHalves || dim0 < a.rot;     // rot is a multiple of 16: all dims of a lane or none
   const bool second = PAIRS != kAdjacent && dim0 >= half;
-  constexpr int F = PAIRS == kAnyHalves ? N : N / 2;       // angles that a lane forms
-  const int f0 = PAIRS == kAdjacent ? dim0 / 2
-                 : PAIRS == kHalves ? dim0 - (second ? half - N / 2 : 0) : dim0 - (second ? half : 0);
+  constexpr int F = N / 2;                 // angles that a lane forms, of its own pairs or half of its and its mate's
+  const int f0 = PAIRS == kAdjacent ? dim0 / 2 : dim0 - (second ? half - F : 0);
   float freq[F];
 #pragma unroll
   for (int j = 0; j < F; ++j) freq[j] = turns ? a.freq[f0 + j] : 0.f;
@@ -163,6 +162,12 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
     const double t = static_cast<double>(pos) * (static_cast<double>(freq[j]) * 0.31830988618379067154);
     sincospif(static_cast<float>(t - 2.0 * rint(0.5 * t)), &s, &c);
   };
+  // The value of the lane that holds the pairs' other dims.
+  const int mate = PAIRS != kAnyHalves || !turns ? lane : second ? lane - half / N : lane + half / N;
+  auto other = [&](float v) {
+    if constexpr (PAIRS == kHalves) return __uint_as_float(xor_lane<L / 2>(__float_as_uint(v)));
+    else return __shfl(v, mate);
+  };
   float cs[N], sn[N];                      // dims that do not turn: frequency 0
 #pragma unroll
   for (int j = 0; j < F; ++j) {
@@ -172,20 +177,14 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
       cs[2 * j] = cs[2 * j + 1] = c;
       sn[2 * j] = -s;
       sn[2 * j + 1] = s;
-    } else if constexpr (PAIRS == kHalves) {
-      // The two lanes of a pair form half of its angles each.
-      const float oc = __uint_as_float(xor_lane<L / 2>(__float_as_uint(c)));
-      const float os = __uint_as_float(xor_lane<L / 2>(__float_as_uint(s)));
+    } else {
+      const float oc = other(c), os = other(s);
       cs[j] = second ? oc : c;
       cs[j + F] = second ? c : oc;
       sn[j] = second ? os : -s;
       sn[j + F] = second ? s : -os;
-    } else {
-      cs[j] = c;
-      sn[j] = second ? s : -s;
     }
   }
-  const int mate = PAIRS != kAnyHalves || !turns ? lane : second ? lane - half / N : lane + half / N;
   T* const dst0 = static_cast<T*>(a.dst[0]) + row * a.ld_dst[0];
   T* const dst1 = static_cast<T*>(a.dst[1]) + row * a.ld_dst[1];
   for (int s = s0; s < s1; s += U) {
@@ -222,8 +221,7 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
       for (int j = 0; j < N; ++j) {
         float m;                           // the pair's other
         if constexpr (PAIRS == kAdjacent) m = x[j ^ 1];
-        else if constexpr (PAIRS == kHalves) m = __uint_as_float(xor_lane<L / 2>(__float_as_uint(x[j])));
-        else m = __shfl(x[j], mate);
+        else m = other(x[j]);
         y[j] = r * (turns ? fmaf(x[j], cs[j], m * sn[j]) : x[j]);
       }
       if (ok) *reinterpret_cast<uint4*>((keys ? dst1 : dst0) + at) = P::narrow(y);
