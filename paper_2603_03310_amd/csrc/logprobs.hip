@@ -79,6 +79,7 @@ __device__ __forceinline__ u64 lp_key(float x, int i) {
 template <typename T, bool STREAM>
 struct Row {
   static constexpr int N = 16 / sizeof(T);
+  static constexpr int kDrop = 32 - 8 * static_cast<int>(sizeof(T));
   const T* base;     // the row's first element
   int shift, V;
   __device__ __forceinline__ Row(const T* b, int v) : base(b), shift(static_cast<int>((reinterpret_cast<uintptr_t>(b) & 15) / sizeof(T))), V(v) {}
@@ -105,16 +106,30 @@ struct Row {
     return make_uint4(v.x, v.y, v.z, v.w);
   }
   // Any piece; elements outside the row read as -inf.
-  __device__ __forceinline__ void load(int p, float (&x)[N]) const {
-    if (whole(p)) {
-      widen(raw(p), x);
-    } else {
+  __device__ __forceinline__ uint4 piece(int p) const {
+    if (whole(p)) return raw(p);
+    unsigned w[4];
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int i = p * N + j - shift;
-        x[j] = i >= 0 && i < V ? value(base[i]) : -INFINITY;
+    for (int j = 0; j < 4; ++j) {
+      constexpr int E = N / 4;                             // elements of a word
+      w[j] = 0u;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int i = p * N + j * E + e - shift;
+        unsigned bits = N == 4 ? 0xff800000u : 0xff80u;
+        if (i >= 0 && i < V) {
+          if constexpr (N == 4) bits = __float_as_uint(base[i]);
+          else bits = base[i];
+        }
+        w[j] |= bits << (32 / E * e);
       }
     }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ void load(int p, float (&x)[N]) const { widen(piece(p), x); }
+  static __device__ __forceinline__ uint4 nothing() {
+    const unsigned w = N == 4 ? 0xff800000u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
   }
 };
 
@@ -177,19 +192,20 @@ struct LpShared {
 // A bound that at least n of a wave's keys (K a lane, distinct but for 0, which is none)
 // reach, and at most `most` >= n of them: by bisection, first over the upper words, then,
 // where too many share the n-th's, over the lower words of those.  All keys but 0 where
-// they are no more than `most`, and anything where they are fewer than n.
-template <int K>
+// they are no more than `most`, and anything where they are fewer than n.  DROP: bits of
+// the upper words that no two logits differ in alone (16 for bf16).
+template <int DROP, int K>
 __device__ __forceinline__ u64 lp_bound(const u64 (&key)[K], int n, int most) {
   unsigned hi[K], top = 0u, least = 0xffffffffu;
   int there = 0;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    hi[k] = static_cast<unsigned>(key[k] >> 32);
+    hi[k] = static_cast<unsigned>(key[k] >> 32) >> DROP;
     top = max(top, hi[k]);
     if (key[k] != 0ull) least = min(least, hi[k]);
     there += static_cast<int>(__popcll(__ballot(key[k] != 0ull)));
   }
-  if (there <= most) return there < n ? 1ull : static_cast<u64>(wave_min_u(least)) << 32;
+  if (there <= most) return there < n ? 1ull : static_cast<u64>(wave_min_u(least)) << (32 + DROP);
   auto count = [&](unsigned from) {
     int c = 0;
 #pragma unroll
@@ -212,7 +228,7 @@ __device__ __forceinline__ u64 lp_bound(const u64 (&key)[K], int n, int most) {
       end = mid;
     }
   }
-  if (c <= most) return static_cast<u64>(lo) << 32;
+  if (c <= most) return static_cast<u64>(lo) << (32 + DROP);
   // Too many at lo itself: the largest lower words among them.
   const int need = n - count(lo + 1u);
   auto ties = [&](unsigned from) {
@@ -222,10 +238,11 @@ __device__ __forceinline__ u64 lp_bound(const u64 (&key)[K], int n, int most) {
       t += static_cast<int>(__popcll(__ballot(hi[k] == lo && static_cast<unsigned>(key[k]) >= from)));
     return t;
   };
-  unsigned first = 0xffffffffu, last = 0u;
+  unsigned first = 0xffffffffu, last = 0u, same = 0u;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     if (hi[k] == lo) {
+      same = static_cast<unsigned>(key[k] >> 32);
       first = min(first, static_cast<unsigned>(key[k]));
       last = max(last, static_cast<unsigned>(key[k]));
     }
@@ -233,13 +250,14 @@ __device__ __forceinline__ u64 lp_bound(const u64 (&key)[K], int n, int most) {
   unsigned low = wave_min_u(first), past = wave_max_u(last);   // at least `need` reach low
   low = __builtin_amdgcn_readfirstlane(low);
   past = __builtin_amdgcn_readfirstlane(past);
-  if (ties(past) >= need) return static_cast<u64>(lo) << 32 | past;
+  same = wave_max_u(same);                     // the upper word that they share
+  if (ties(past) >= need) return static_cast<u64>(same) << 32 | past;
   while (past - low > 1u) {
     const unsigned mid = low + (past - low) / 2u;
     if (ties(mid) >= need) low = mid;
     else past = mid;
   }
-  return static_cast<u64>(lo) << 32 | low;
+  return static_cast<u64>(same) << 32 | low;
 }
 
 // The n largest of sh.cand[0 .. cand) by counting: f(rank, key).
@@ -270,7 +288,7 @@ __device__ __forceinline__ void lp_largest(const LpArgs& a, LpShared& sh, const 
     u64 key[NT / 64];
 #pragma unroll
     for (int k = 0; k < NT / 64; ++k) key[k] = sh.key[k * 64 + lane];
-    const u64 e = lp_bound(key, n, n + n / 2 + 3);
+    const u64 e = lp_bound<R::kDrop>(key, n, n + n / 2 + 3);
     if (lane == 0) sh.edge = e;
   }
   __syncthreads();
@@ -342,6 +360,7 @@ __device__ __forceinline__ void lp_largest(const LpArgs& a, LpShared& sh, const 
 // A row's outputs from its parts' sums and descending lists, by one workgroup.  A bound
 // that n keys reach: the n-th largest of the lists' first keys, or, of fewer lists, the
 // least of their q-th, where q entries of each are n.
+template <int DROP>
 __device__ __forceinline__ void lp_join(const LpArgs& a, LpShared& sh, int row, const LpScale& sc, int tok,
                                         float z) {
   constexpr int NT = kLpThreads, K = kLpParts * kLpTop / NT;
@@ -371,7 +390,7 @@ __device__ __forceinline__ void lp_join(const LpArgs& a, LpShared& sh, int row, 
       u64 e;
       if (q == 1) {
         const u64 one[1] = {head};
-        e = lp_bound(one, n, n);
+        e = lp_bound<DROP>(one, n, n);
       } else {
         const u64 mine = t < a.parts ? head : ~0ull;
         const unsigned hi = wave_min_u(static_cast<unsigned>(mine >> 32));
@@ -416,7 +435,9 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs a) {
 
   float mx = -INFINITY, s = 0.f, w = 0.f;
   int mp = p0 + t;                         // first piece that holds mx
-  auto take = [&](const float (&x)[N], int p) {
+  auto take = [&](uint4 v, int p) {
+    float x[N];
+    R::widen(v, x);
     float b = x[0];
 #pragma unroll
     for (int j = 1; j < N; ++j) b = fmaxf(b, x[j]);
@@ -439,17 +460,18 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs a) {
   };
   // The walk, in segments of `rounds` steps.
   const int rounds = (p1 - p0 + U * NT * kLpSegs - 1) / (U * NT * kLpSegs);
+  const int in0 = r.shift ? 1 : 0, in1 = min(p1, (a.V + r.shift) / N);      // whole pieces of the part
   for (int g = 0, p = p0 + t; p - t < p1; ++g) {
     float top = -INFINITY;
     for (int k = 0; k < rounds; ++k, p += U * NT) {
-      float x[U][N];
+      uint4 x[U];
+      // Steps inside the row without a test per piece.
+      if (p - t >= in0 && p - t + U * NT <= in1) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (p + u * NT < p1) r.load(p + u * NT, x[u]);
-        else {
+        for (int u = 0; u < U; ++u) x[u] = r.raw(p + u * NT);
+      } else {
 #pragma unroll
-          for (int j = 0; j < N; ++j) x[u][j] = -INFINITY;
-        }
+        for (int u = 0; u < U; ++u) x[u] = p + u * NT < p1 ? r.piece(p + u * NT) : R::nothing();
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) top = fmaxf(top, take(x[u], p + u * NT));
@@ -508,7 +530,7 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs a) {
   __syncthreads();
   if (!sh.last) return;
   if (t == 0) a.tickets[row] = 0u;
-  lp_join(a, sh, row, sc, tok, z);
+  lp_join<R::kDrop>(a, sh, row, sc, tok, z);
 }
 
 }  // namespace
