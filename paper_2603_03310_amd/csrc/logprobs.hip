@@ -32,7 +32,7 @@ namespace {
 
 constexpr int kLpThreads = 256;
 constexpr int kLpTop = ENT_MAX_TOP_LOGPROBS;
-constexpr int kLpCand = 1024;         // candidates that are ranked at once
+constexpr int kLpCand = 1024;         // candidates that are ranked at once (a wave alone: a quarter)
 constexpr int kLpParts = 64;          // parts of a row, at most
 constexpr int kLpWho = 64;            // threads that can reach the bound
 constexpr int kLpSegs = 8;            // segments of a thread's walk
@@ -176,13 +176,15 @@ __device__ __forceinline__ V lp_shared(const V* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+template <int NT>
 struct LpShared {
-  u64 key[kLpThreads];       // per thread: its largest logit (of its maxima, first piece)
+  static constexpr int kCand = NT == kLpThreads ? kLpCand : kLpCand / 4;
+  u64 key[NT];               // per thread: its largest logit (of its maxima, first piece)
   union {
-    float seg[kLpSegs][kLpThreads]; // ... in each segment, until `again` is made of it
-    u64 cand[kLpCand];
+    float seg[kLpSegs][NT];         // ... in each segment, until `again` is made of it
+    u64 cand[kCand];
   };
-  float red[3 * kLpThreads / 64];
+  float red[3 * NT / 64];
   int again[kLpWho * kLpSegs];      // (segment, thread) that are read again
   u64 edge;
   int count, agains, last;
@@ -261,9 +263,9 @@ __device__ __forceinline__ u64 lp_bound(const u64 (&key)[K], int n, int most) {
 }
 
 // The n largest of sh.cand[0 .. cand) by counting: f(rank, key).
-template <typename F>
-__device__ __forceinline__ void lp_rank(const LpShared& sh, int cand, int n, F f) {
-  for (int i = threadIdx.x; i < cand; i += kLpThreads) {
+template <int NT, typename F>
+__device__ __forceinline__ void lp_rank(const LpShared<NT>& sh, int cand, int n, F f) {
+  for (int i = threadIdx.x; i < cand; i += NT) {
     const u64 mine = sh.cand[i];
     int rank = 0;
     for (int k = 0; k < cand; ++k) rank += sh.cand[k] > mine ? 1 : 0;
@@ -273,10 +275,10 @@ __device__ __forceinline__ void lp_rank(const LpShared& sh, int cand, int n, F f
 
 // The n largest logits of pieces [p0, p1), `per` pieces of a thread in a segment, given
 // the threads' largest in sh.key and sh.seg.
-template <typename R>
-__device__ __forceinline__ void lp_largest(const LpArgs& a, LpShared& sh, const R& r, int p0, int p1, int per,
+template <typename R, int NT>
+__device__ __forceinline__ void lp_largest(const LpArgs& a, LpShared<NT>& sh, const R& r, int p0, int p1, int per,
                                            int row, float c) {
-  constexpr int N = R::N, NT = kLpThreads;
+  constexpr int N = R::N;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, n = a.n_top;
   const bool whole = a.parts == 1;
   auto put = [&](int rank, u64 key) {
@@ -317,14 +319,14 @@ __device__ __forceinline__ void lp_largest(const LpArgs& a, LpShared& sh, const 
         const int i = p * N + j - r.shift;
         if (counts(x[j], i, p)) {
           const int at = atomicAdd(&sh.count, 1);
-          if (at < kLpCand) sh.cand[at] = lp_key(x[j], i);
+          if (at < sh.kCand) sh.cand[at] = lp_key(x[j], i);
         }
       }
     }
   }
   __syncthreads();
   const int cand = sh.count;
-  if (cand <= kLpCand) {
+  if (cand <= sh.kCand) {
     lp_rank(sh, cand, n, put);
     // A part shorter than n, or a row with NaN.
     for (int i = cand + t; i < n; i += NT) put(i, 0ull);
@@ -361,7 +363,7 @@ __device__ __forceinline__ void lp_largest(const LpArgs& a, LpShared& sh, const 
 // that n keys reach: the n-th largest of the lists' first keys, or, of fewer lists, the
 // least of their q-th, where q entries of each are n.
 template <int DROP>
-__device__ __forceinline__ void lp_join(const LpArgs& a, LpShared& sh, int row, const LpScale& sc, int tok,
+__device__ __forceinline__ void lp_join(const LpArgs& a, LpShared<kLpThreads>& sh, int row, const LpScale& sc, int tok,
                                         float z) {
   constexpr int NT = kLpThreads, K = kLpParts * kLpTop / NT;
   const int t = threadIdx.x, n = a.n_top, total = a.parts * n;
@@ -415,12 +417,13 @@ __device__ __forceinline__ void lp_join(const LpArgs& a, LpShared& sh, int row, 
   for (int i = cand + t; i < n; i += NT) put(i, 0ull);         // a row with NaN
 }
 
-template <typename T, bool STREAM>
-__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs a) {
+// NT: threads of a workgroup; 64 take whole rows only.
+template <typename T, bool STREAM, int NT>
+__global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs a) {
   using R = Row<T, STREAM>;
-  constexpr int N = R::N, NT = kLpThreads;
+  constexpr int N = R::N;
   constexpr int U = STREAM ? 8 : 4;        // pieces of a thread in flight
-  __shared__ LpShared sh;
+  __shared__ LpShared<NT> sh;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
   const int tok = a.tokens ? a.tokens[row] : 0;
@@ -521,16 +524,18 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs a) {
   if (n > 0) lp_largest(a, sh, r, p0, p1, rounds * U, row, sc.c);
   if (whole) return;
 
-  // The row's last part joins them all.
-  __builtin_amdgcn_s_waitcnt(0);         // this wave's device-scope stores have completed
-  __syncthreads();
-  if (t == 0)
-    sh.last = __hip_atomic_fetch_add(a.tickets + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-              static_cast<unsigned>(a.parts) - 1u;
-  __syncthreads();
-  if (!sh.last) return;
-  if (t == 0) a.tickets[row] = 0u;
-  lp_join<R::kDrop>(a, sh, row, sc, tok, z);
+  if constexpr (NT == kLpThreads) {
+    // The row's last part joins them all.
+    __builtin_amdgcn_s_waitcnt(0);         // this wave's device-scope stores have completed
+    __syncthreads();
+    if (t == 0)
+      sh.last = __hip_atomic_fetch_add(a.tickets + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                static_cast<unsigned>(a.parts) - 1u;
+    __syncthreads();
+    if (!sh.last) return;
+    if (t == 0) a.tickets[row] = 0u;
+    lp_join<R::kDrop>(a, sh, row, sc, tok, z);
+  }
 }
 
 }  // namespace
@@ -566,9 +571,19 @@ hipError_t launch_token_logprobs(const ent_ctx* c, int T, const void* logits, in
   const int part16 = static_cast<int>((bytes + 16383) / 16384);
   a.parts = std::max(1, std::min({kLpParts, kLpSlots / T, std::max(std::min(c->num_cu / T, part16), (part16 + 1) / 2)}));
   const bool stream = bytes * T > kLpStream;
-  auto kern = bf16 ? (stream ? logprobs_kernel<uint16_t, true> : logprobs_kernel<uint16_t, false>)
-                   : (stream ? logprobs_kernel<float, true> : logprobs_kernel<float, false>);
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(T) * a.parts), dim3(kLpThreads), 0, s, a);
+  // Short rows, and many of some length, to a wave each instead of to four: what a row
+  // costs besides its reads is then four times as cheap, and rows are enough to fill the
+  // GPU.  Us (n_top 5): 20000 rows of 1000 floats 26.4 against 66.5, of 8000 bf16 78
+  // against 127, 5000 of 8000 floats 35.0 against 38.9, but 1000 of them 14.2 against 11.3
+  // and 5000 of 16000 floats 66.9 against 62.5.
+  const bool alone = a.parts == 1 && (bytes <= 4 << 10 || (bytes <= 32 << 10 && T >= 8 * c->num_cu));
+  auto kern = bf16 ? (alone    ? logprobs_kernel<uint16_t, false, 64>
+                      : stream ? logprobs_kernel<uint16_t, true, kLpThreads>
+                               : logprobs_kernel<uint16_t, false, kLpThreads>)
+                   : (alone    ? logprobs_kernel<float, false, 64>
+                      : stream ? logprobs_kernel<float, true, kLpThreads>
+                               : logprobs_kernel<float, false, kLpThreads>);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(T) * a.parts), dim3(alone ? 64 : kLpThreads), 0, s, a);
   return hipGetLastError();
 }
 
