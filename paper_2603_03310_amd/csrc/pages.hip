@@ -13,15 +13,12 @@
 
 #include <algorithm>
 
-#ifndef KDENSE
-#define KDENSE 8
-#endif
 namespace ent {
 namespace {
 
 constexpr int kPageThreads = 256;
 constexpr int kPlanThreads = 1024;
-constexpr int kDense = KDENSE;          // bits of a word, on average, that a wave writes together
+constexpr int kDense = 8;               // bits of a word, on average, that a wave writes together
 constexpr int kBitPitch = kPageBitBytes / 8;     // 64-bit words from one word of a bitmap to the next
 
 // Where a block's contents lie: caches of tile_bytes a block, mean keys, scales.
@@ -57,27 +54,24 @@ __device__ __forceinline__ void copy_units(const uint4* __restrict__ s, uint4* _
   for (; i < units; i += nt) d[i] = s[i];
 }
 
-// Block `from`'s contents to block `to` by threads t of nt: U pieces of keys and U of
+// Block `from`'s contents to block `to` by threads t of nt: two pieces of keys and two of
 // values in flight a thread.
-template <int U>
 __device__ __forceinline__ void copy_block(const PageStore& st, int from, int to, int t, int nt) {
   const uint4 *sk = at16(static_cast<const void*>(st.k), from * st.tile_bytes), *sv = at16(static_cast<const void*>(st.v), from * st.tile_bytes);
   uint4 *dk = at16(st.k, to * st.tile_bytes), *dv = at16(st.v, to * st.tile_bytes);
   const int units = static_cast<int>(st.tile_bytes / 16);
-  for (int i = t; i < units; i += U * nt) {
-    uint4 x[U], y[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * nt < units) {
-        x[u] = sk[i + u * nt];
-        y[u] = sv[i + u * nt];
-      }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * nt < units) {
-        dk[i + u * nt] = x[u];
-        dv[i + u * nt] = y[u];
-      }
+  int i = t;
+  for (; i + nt < units; i += 2 * nt) {
+    const uint4 x = sk[i], y = sv[i], x1 = sk[i + nt], y1 = sv[i + nt];
+    dk[i] = x;
+    dv[i] = y;
+    dk[i + nt] = x1;
+    dv[i + nt] = y1;
+  }
+  for (; i < units; i += nt) {
+    const uint4 x = sk[i], y = sv[i];
+    dk[i] = x;
+    dv[i] = y;
   }
   if (st.ksum)
     copy_units<1>(at16(static_cast<const void*>(st.ksum), 4ll * from * st.sum_floats),
@@ -145,14 +139,14 @@ __device__ __forceinline__ int bits_below(u64 b) {
   return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(b >> 32),
                                                     __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(b), 0u)));
 }
-__device__ __forceinline__ bool bit_here(u64 b) { return (b >> (threadIdx.x & 63) & 1ull) != 0; }
+__device__ __forceinline__ bool bit_here(u64 b) { return __builtin_amdgcn_inverse_ballot_w64(b); }
 // A workgroup's words (word t of thread t, `n` of them), each with a value: f(word, value,
 // t) by all lanes of a wave, lane l for bit l, with consecutive words dealt to the waves and
-// four of them together (one after the other, a word is a chain of some 25 instructions:
+// eight of them together (one after the other, a word is a chain of some 25 instructions:
 // 120 ns).  s_b, s_v: a place per thread.
 template <int NT, typename F>
 __device__ __forceinline__ void each_word(u64 b, int v, int n, u64* s_b, int* s_v, F f) {
-  constexpr int W = NT / 64, Q = 4;
+  constexpr int W = NT / 64, Q = 8;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   s_b[t] = b;
   s_v[t] = v;
@@ -222,8 +216,8 @@ struct ForkArgs {
 };
 
 // What every fork does: emit(i, record).  Returns the free list's new lower end (its
-// old one where the range is bad).  mem: R + (R + 31) / 32 ints.
-template <int NT, typename F>
+// old one where the range is bad).  mem: R + (R + 31) / 32 ints.  ONE: N <= NT.
+template <int NT, bool ONE, typename F>
 __device__ __forceinline__ int fork_plan(const ForkArgs& a, int* mem, unsigned& bad, F emit) {
   __shared__ int s_red[NT / 64];
   __shared__ int s_cut;
@@ -238,7 +232,7 @@ __device__ __forceinline__ int fork_plan(const ForkArgs& a, int* mem, unsigned& 
   if (t == 0) s_cut = ring_ok ? 0x7fffffff : 0;
   __syncthreads();
   auto row_ok = [&](int r) { return r >= 0 && r < a.tb.R; };
-  const int per = (a.N + NT - 1) / NT;       // consecutive forks of a thread
+  const int per = ONE ? 1 : (a.N + NT - 1) / NT;       // consecutive forks of a thread
   for (int k = 0; k < per; ++k) {
     const int i = t * per + k;
     if (i < a.N) {
@@ -304,7 +298,7 @@ __device__ __forceinline__ int fork_plan(const ForkArgs& a, int* mem, unsigned& 
 __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkArgs a) {
   extern __shared__ int s_mem[];
   unsigned bad = 0;
-  const int head = fork_plan<kPlanThreads>(a, s_mem, bad, [&](int i, int4 r) { a.rec[i] = r; });
+  const int head = fork_plan<kPlanThreads, false>(a, s_mem, bad, [&](int i, int4 r) { a.rec[i] = r; });
   if (threadIdx.x == 0) a.range[0] = head;
   if (bad) raise_flag(a.tb.flags, bad);
 }
@@ -320,7 +314,7 @@ __global__ __launch_bounds__(kPageThreads) void fork_kernel(ForkArgs a) {
   unsigned bad = 0;
   if constexpr (ONE) {
     __shared__ int4 s_rec;
-    head = fork_plan<kPageThreads>(a, s_mem, bad, [&](int i, int4 x) { if (i == fork) s_rec = x; });
+    head = fork_plan<kPageThreads, true>(a, s_mem, bad, [&](int i, int4 x) { if (i == fork) s_rec = x; });
     // Every workgroup finds the same; the first raises it.
     if (blockIdx.x != 0) bad = 0;
     __syncthreads();                        // the free list's range has been read
@@ -348,7 +342,7 @@ __global__ __launch_bounds__(kPageThreads) void fork_kernel(ForkArgs a) {
       const int t = (part - a.row_parts) * kPageThreads + threadIdx.x;
       if (!ok || !there) bad |= ENT_DEV_BAD_TABLE;
       if (t == 0) to[full] = ok ? id : -1;
-      if (ok && there) copy_block<2>(a.st, p, id, t, (a.parts - a.row_parts) * kPageThreads);
+      if (ok && there) copy_block(a.st, p, id, t, (a.parts - a.row_parts) * kPageThreads);
     }
   }
   if (bad) raise_flag(a.tb.flags, bad);
