@@ -225,3 +225,15 @@ def test_refusals(torch_cuda):
             dec.logprobs(z.t().contiguous().t(), tk, lp)
         torch.cuda.synchronize()
         assert (lp == -7.0).all().item()
+
+
+def test_offsets_past_32_bits(torch_cuda):
+    """Rows that lie more than 2^32 elements into their buffer."""
+    torch = torch_cuda
+    rng = np.random.default_rng(12)
+    V, ld, T = 1001, 1 << 30, 6
+    buf = torch.empty((T - 1) * ld + V, dtype=torch.bfloat16, device="cuda:0")
+    z = torch.as_strided(buf, (T, V), (ld, 1))
+    z.copy_(torch.tensor(rng.normal(size=(T, V)) * 3, device="cuda:0"))
+    tokens = rng.integers(0, V, T)
+    check(z, run(torch, z, tokens, 5), tokens, 5)

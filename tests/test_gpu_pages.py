@@ -322,3 +322,51 @@ def test_refusals(torch_cuda):
     with decoder(q) as dec:                                     # 8-bit codes need a bf16 context
         refused(dec, unsup, "fork", ks=sc, vs=sc)
         refused(dec, unsup, "compact", ks=sc, vs=sc)
+
+
+def test_offsets_past_32_bits(torch_cuda):
+    """Blocks that lie more than 4 GB into their cache, forked, compacted and freed."""
+    torch = torch_cuda
+    P, H, D = 140000, 8, 128                                     # 4.6 GB of keys, as many of values
+    p = Pool(torch, [20, 40, 16], 5, 300, 4, "bf16", H, D, seed=10)
+    order = np.random.default_rng(11).permutation(300) + P - 300
+    p.tables = np.where((p.tables >= 0) & (p.tables < 300), order[p.tables % 300], p.tables)
+    p.ids = np.concatenate([np.zeros(P - 300, np.int64), order[p.ids]])
+    p.free, p.P = [P - 300 + p.free[0], P], P
+    p.shared = np.zeros(P, np.int64)
+    p.cfg["num_pool_blocks"] = P
+    small = p.pools
+    wide = [torch.zeros((P,) + x.shape[1:], dtype=torch.tensor(x[:1]).dtype, device="cuda:0") for x in small]
+    for w, x in zip(wide, small):
+        w[P - 300:] = torch.tensor(x, device="cuda:0")
+
+    class Blocks:                                                # the host's copy of the few blocks that matter
+        def __init__(self, x):
+            self.at = {P - 300 + i: x[i].copy() for i in range(300)}
+
+        def __getitem__(self, i):
+            return self.at[int(i)]
+
+        def __setitem__(self, i, v):
+            self.at[int(i)] = np.array(v)
+
+    hosts = [Blocks(x) for x in small]
+    p.pools = []
+    p.upload()
+    p.pools, p.dp = hosts, wide
+
+    def same():
+        for name in ("tables", "ctx", "shared", "ids", "free"):
+            assert np.array_equal(p.d[name].cpu().numpy(), np.asarray(getattr(p, name))), name
+        for h, w in zip(hosts, wide):
+            ids = sorted(h.at)
+            got = w[torch.tensor(ids, device="cuda:0")].cpu().numpy()
+            assert np.array_equal(got, np.stack([h.at[i] for i in ids]))
+
+    p.same = same
+    with decoder(p) as dec:
+        p.both(dec, "fork", [0, 1], [3, 4], flags=0)
+        p.both(dec, "release", [1], flags=0)
+        p.both(dec, "compact", flags=0)
+        assert p.count == 7 and max(h for h in hosts[0].at) >= P - 300 and 0 in hosts[0].at
+        p.both(dec, "release", [0, 2, 3, 4], flags=0)

@@ -219,3 +219,24 @@ def test_refusals(torch_cuda):
         # Beside each other in one projection's rows is no overlap.
         call(dec, qo=rows[:, 6:10], ko=rows[:, 10:12])
         torch.cuda.synchronize()
+
+
+def test_offsets_past_32_bits(torch_cuda):
+    """Rows that lie more than 2^32 elements into their buffers, at the largest row stride."""
+    torch = torch_cuda
+    rng = np.random.default_rng(13)
+    T, ld = 300, 1 << 24
+    buf = torch.empty((T - 1) * ld + 8 * 64, dtype=torch.bfloat16, device="cuda:0")
+    rows = torch.as_strided(buf, (T, 8, 64), (ld, 64, 1))
+    q, k, qx, kx = data(torch, rng, T, 2, 2, 64, "bf16", False)
+    rows[:, :2], rows[:, 2:4] = q, k
+    prm, g = params(torch, rng, 64, 64, False, (1, 1))
+    from paper_2603_03310_amd.runner import Decoder
+    with Decoder(**config(2, 2, 64, max_batch=T)) as dec:
+        ctx = torch.arange(T, dtype=torch.int32, device="cuda:0")
+        dec.rotate(T, prm, rows[:, :2], rows[:, 2:4], rows[:, 4:6], rows[:, 6:8], ctx_lens=ctx)
+        torch.cuda.synchronize()
+    got = host(rows)
+    check(got[:, 4:6], qx, got[:, 4:6], np.arange(T), g[0], freqs(64), 1e-5, 64, False, "bf16")
+    check(got[:, 6:8], kx, got[:, 6:8], np.arange(T), g[1], freqs(64), 1e-5, 64, False, "bf16")
+    assert np.array_equal(got[:, :2], qx) and np.array_equal(got[:, 2:4], kx)
