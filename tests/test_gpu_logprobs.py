@@ -237,3 +237,42 @@ def test_offsets_past_32_bits(torch_cuda):
     z.copy_(torch.tensor(rng.normal(size=(T, V)) * 3, device="cuda:0"))
     tokens = rng.integers(0, V, T)
     check(z, run(torch, z, tokens, 5), tokens, 5)
+
+
+def test_two_graphs_and_another_stream(torch_cuda):
+    """Two graphs of one context, with rows in parts and rows that are not, replayed in turn with
+    eager calls between; and a call on another stream."""
+    torch = torch_cuda
+    from paper_2603_03310_amd.runner import Decoder
+    rng = np.random.default_rng(14)
+    V = 40001
+    zs = [rows(torch, rng, 3, V, "f32"), rows(torch, rng, 1030, V, "bf16")]
+    tk = [torch.tensor(rng.integers(0, V, len(z)), dtype=torch.int32, device="cuda:0") for z in zs]
+    f = lambda *s: torch.zeros(*s, device="cuda:0")  # noqa: E731
+    outs = [(f(len(z)), f(len(z)), torch.zeros((len(z), 7), dtype=torch.int32, device="cuda:0"), f(len(z), 7)) for z in zs]
+    with Decoder(**config(8, 8, 64, vocab=V, log_v=20.0)) as dec:
+        graphs, want = [], []
+        for z, t, o in zip(zs, tk, outs):
+            dec.logprobs(z, t, *o)
+            torch.cuda.synchronize()
+            want.append([x.clone() for x in o])
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+                dec.logprobs(z, t, *o)
+            graphs.append(g)
+        for _ in range(3):
+            for i in (0, 1, 1, 0):
+                for x in outs[i]:
+                    x.zero_()
+                graphs[i].replay()
+                torch.cuda.synchronize()
+                assert all(torch.equal(x, w) for x, w in zip(outs[i], want[i]))
+                dec.logprobs(zs[1 - i][:2], tk[1 - i][:2], *(x[:2] for x in outs[1 - i]))
+                torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        for x in outs[0]:
+            x.zero_()
+        s.wait_stream(torch.cuda.current_stream())
+        dec.logprobs(zs[0], tk[0], *outs[0], stream=s)
+        s.synchronize()
+        assert all(torch.equal(x, w) for x, w in zip(outs[0], want[0]))

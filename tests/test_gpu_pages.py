@@ -55,6 +55,8 @@ class Pool:
         i32 = lambda x: self.torch.tensor(np.asarray(x), dtype=self.torch.int32, device="cuda:0")  # noqa: E731
         sh = d["shared"] if shared else None
         rows = [i32(r) for r in rows]
+        if stream is not None:
+            self.torch.cuda.synchronize()
         if what == "fork":
             dec.fork(*rows, d["tables"], d["ctx"], sh, d["ids"], d["free"], k, v, ksum, *sc, stream=stream)
         elif what == "release":
@@ -270,6 +272,19 @@ def test_captured_and_replayed(torch_cuda):
             dec.release(i32([4]), d["tables"], d["ctx"], d["ids"], d["free"], d["shared"])
             torch.cuda.synchronize()
         assert dec.device_status() == 0
+
+
+def test_another_stream(torch_cuda):
+    torch = torch_cuda
+    p = Pool(torch, [100, 60, 16, 3], 8, 60, 8, seed=15)
+    p.upload()
+    s = torch.cuda.Stream()
+    with decoder(p) as dec:
+        for what, rows in (("fork", ([0, 1, 0], [4, 5, 6])), ("release", ([0, 2, 5],)), ("compact", ())):
+            assert p.oracle(what, *rows) == 0
+            s.wait_stream(torch.cuda.current_stream())
+            p.call(dec, what, *rows, stream=s)
+            p.same()
 
 
 def test_refusals(torch_cuda):
