@@ -18,6 +18,7 @@ constexpr int kMinTickets = 1024;           // counters in the workspace, at lea
 constexpr int kMaxBlocksPerSeq = 16384;     // selection keeps all scores in LDS
 constexpr int kEstChunkThreads = 256;       // threads of an entropy chunk job (maxima per chunk)
 constexpr int kPageBitBytes = 64;           // from one word of the block bitmap to the next
+constexpr long long kStreamBytes = 256ll << 20;   // traffic of a launch past what the last-level cache holds
 constexpr int kLpSlots = 1024;              // parts of the rows that log probabilities are cut into
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -406,6 +407,26 @@ __device__ __forceinline__ float lane_at(float v, int i) {
 __device__ __forceinline__ double lane_at(double v, int i) {
   const int2 u = __builtin_bit_cast(int2, v);
   return __builtin_bit_cast(double, make_int2(lane_at(u.x, i), lane_at(u.y, i)));
+}
+
+// 16 bytes; STREAM: without a place in the caches.
+template <bool STREAM>
+__device__ __forceinline__ uint4 load16(const void* p) {
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4* q = static_cast<const u32x4*>(p);
+  const u32x4 v = STREAM ? __builtin_nontemporal_load(q) : *q;
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+template <bool STREAM>
+__device__ __forceinline__ void store16(void* p, uint4 x) {
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 v;
+  v.x = x.x;
+  v.y = x.y;
+  v.z = x.z;
+  v.w = x.w;
+  if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+  else *static_cast<u32x4*>(p) = v;
 }
 
 __device__ __forceinline__ void raise_flag(unsigned* flags, unsigned f) {

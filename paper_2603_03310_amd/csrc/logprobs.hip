@@ -39,10 +39,6 @@ constexpr int kLpSegs = 8;            // segments of a thread's walk
 static_assert(kLpTop * kLpTop <= kLpCand, "keys of a row's n lists");
 static_assert(kLpTop + kLpTop / 2 + 3 <= kLpWho, "threads over the bound");
 static_assert(kLpParts == 64 && kLpParts <= kLpThreads, "a wave joins the parts");
-// Logits past what the last-level cache holds are read without a place in the caches:
-// 2500 rows of 128256 floats 238 us against 257 with (then with 8 pieces of a thread in
-// flight 212, with 4 217); 64 rows of bf16 18.8 against 18.4.
-constexpr long long kLpStream = 256ll << 20;
 typedef unsigned long long u64;
 
 struct LpArgs {
@@ -100,10 +96,7 @@ struct Row {
   }
   __device__ __forceinline__ bool whole(int p) const { return p * N >= shift && (p + 1) * N - shift <= V; }
   __device__ __forceinline__ uint4 raw(int p) const {
-    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-    const u32x4* q = reinterpret_cast<const u32x4*>(base + (static_cast<long long>(p) * N - shift));
-    const u32x4 v = STREAM ? __builtin_nontemporal_load(q) : *q;
-    return make_uint4(v.x, v.y, v.z, v.w);
+    return load16<STREAM>(base + (static_cast<long long>(p) * N - shift));
   }
   // Any piece; elements outside the row read as -inf.
   __device__ __forceinline__ uint4 piece(int p) const {
@@ -570,7 +563,10 @@ hipError_t launch_token_logprobs(const ent_ctx* c, int T, const void* logits, in
   const long long bytes = static_cast<long long>(a.V) * (bf16 ? 2 : 4);
   const int part16 = static_cast<int>((bytes + 16383) / 16384);
   a.parts = std::max(1, std::min({kLpParts, kLpSlots / T, std::max(std::min(c->num_cu / T, part16), (part16 + 1) / 2)}));
-  const bool stream = bytes * T > kLpStream;
+  // Logits past what the last-level cache holds are read without a place in the caches: 2500
+  // rows of 128256 floats 238 us against 257 with (202 with 8 pieces of a thread in flight and
+  // steps without tests); 64 rows of bf16 18.8 against 18.4.
+  const bool stream = bytes * T > kStreamBytes;
   // Short rows, and many of some length, to a wave each instead of to four: what a row
   // costs besides its reads is then four times as cheap, and rows are enough to fill the
   // GPU.  Us (n_top 5): 20000 rows of 1000 floats 26.4 against 66.5, of 8000 bf16 78

@@ -43,18 +43,19 @@ __device__ __forceinline__ uint4* at16(void* p, long long byte) {
   return reinterpret_cast<uint4*>(static_cast<char*>(p) + byte);
 }
 
-template <int U>
+// The copy of `units` 16-byte pieces by threads t of nt, U of a thread in flight.
+template <int U, bool STREAM>
 __device__ __forceinline__ void copy_units(const uint4* __restrict__ s, uint4* __restrict__ d, int units, int t,
                                            int nt) {
   int i = t;
   for (; i + (U - 1) * nt < units; i += U * nt) {
     uint4 x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = s[i + u * nt];
+    for (int u = 0; u < U; ++u) x[u] = load16<STREAM>(s + i + u * nt);
 #pragma unroll
-    for (int u = 0; u < U; ++u) d[i + u * nt] = x[u];
+    for (int u = 0; u < U; ++u) store16<STREAM>(d + i + u * nt, x[u]);
   }
-  for (; i < units; i += nt) d[i] = s[i];
+  for (; i < units; i += nt) store16<STREAM>(d + i, load16<STREAM>(s + i));
 }
 
 // Block `from`'s contents to block `to` by threads t of nt: two pieces of keys and two of
@@ -77,7 +78,7 @@ __device__ __forceinline__ void copy_block(const PageStore& st, int from, int to
     dv[i] = y;
   }
   if (st.ksum)
-    copy_units<1>(at16(static_cast<const void*>(st.ksum), 4ll * from * st.sum_floats),
+    copy_units<1, false>(at16(static_cast<const void*>(st.ksum), 4ll * from * st.sum_floats),
                   at16(st.ksum, 4ll * to * st.sum_floats), st.sum_floats / 4, t, nt);
   if (st.ks) {
     for (int i = t; i < st.Hkv; i += nt) {
@@ -448,9 +449,10 @@ __global__ __launch_bounds__(kPlanThreads) void release_kernel(ReleaseArgs a) {
 // free place below U).  A second launch moves contents and counts, and rewrites tables
 // and the free list.  Places that are written (below U, free) and read (from U on) do not
 // meet, so moves are in any order.  Bound by the copies: 5120 moved blocks of 64 KB and
-// their mean keys (713 MB) in 146 us of 157 = 4.9 TB/s, a large copy's rate; the first
+// their mean keys (713 MB) in 126 us of 137 = 5.7 TB/s, over a large copy's 4.7; the first
 // launch's 11 are the chain of round trips and 5 for the lists of moves.  (One workgroup
-// for a block, keys before values, four pieces a thread: 196 us in all.)
+// for a block, keys before values, four pieces a thread: 196 us in all; through the caches
+// 157.)
 // ---------------------------------------------------------------------------
 struct CompactArgs {
   Tables tb;
@@ -552,10 +554,10 @@ __global__ __launch_bounds__(kPageThreads) void compact_kernel(CompactArgs a) {
       const int from = a.from[m >> 1], to = a.to[m >> 1];
       const bool keys = (m & 1) == 0;
       char* const base = keys ? a.st.k : a.st.v;
-      copy_units<8>(at16(static_cast<const void*>(base), from * a.st.tile_bytes), at16(base, to * a.st.tile_bytes),
+      copy_units<8, true>(at16(static_cast<const void*>(base), from * a.st.tile_bytes), at16(base, to * a.st.tile_bytes),
                     units, t, kPageThreads);
       if (keys && a.st.ksum)
-        copy_units<1>(at16(static_cast<const void*>(a.st.ksum), 4ll * from * a.st.sum_floats),
+        copy_units<1, true>(at16(static_cast<const void*>(a.st.ksum), 4ll * from * a.st.sum_floats),
                       at16(a.st.ksum, 4ll * to * a.st.sum_floats), a.st.sum_floats / 4, t, kPageThreads);
       if (a.st.ks) {
         float* sc = keys ? a.st.ks : a.st.vs;
@@ -655,7 +657,11 @@ hipError_t launch_cache_compact(const ent_ctx* c, int R, int* tables, const int*
   if (e != hipSuccess) return e;
   a.parts = row_parts(c, R, kPageThreads);
   a.row_wgs = R * a.parts;
-  hipLaunchKernelGGL(compact_kernel, dim3(a.row_wgs + 8 * c->num_cu), dim3(kPageThreads), 0, s, a);
+  // A workgroup for each half of a move, as far as the pool could have as many, up to 32 a CU
+  // (5120 moves, us with 3 / 5 / 8 / 16 / 32 a CU: 142.5 / 143.9 / 145.5 / 140.7 / 137.4).
+  const long long halves = std::min<long long>(c->cfg.num_pool_blocks, 2ll * R * c->cfg.max_blocks_per_seq);
+  const int copiers = static_cast<int>(std::min<long long>(std::max(halves, 1ll), 32ll * c->num_cu));
+  hipLaunchKernelGGL(compact_kernel, dim3(a.row_wgs + copiers), dim3(kPageThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -10,8 +10,8 @@
 // meet by lane moves, else by shuffles, and the two lanes form half of the angles each.
 //
 // Bound by memory, each row read and written once: 51624 rows of 64 + 8 heads of 128
-// (bf16, 1.90 GB) 369 us = 5.15 TB/s, a little over a large copy's rate.  On the way
-// there: four waves a row, each with all of its angles and a shuffle per value, 956 us.
+// (bf16, 1.90 GB) 329 us = 5.8 TB/s, over a large copy's 4.7.  On the way there: four
+// waves a row, each with all of its angles and a shuffle per value, 956 us.
 // Few rows are a chain of round trips (starts, length, then sines): 128 rows 5.1 us with
 // frequencies and gains loaded before the position is known, 6.8 with them after.
 
@@ -99,13 +99,13 @@ struct Piece {
 // head away (all dims turn in pairs of halves), or some other.
 enum { kAdjacent, kHalves, kAnyHalves };
 
-template <typename T, int D, int PAIRS>
+template <typename T, int D, int PAIRS, bool STREAM>
 __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
   using P = Piece<T>;
   constexpr int N = P::N;
   constexpr int L = D / N;                 // lanes of a head
   constexpr int H = 64 / L;                // heads of a wave's step
-  constexpr int U = 3;                     // steps whose loads are in flight together
+  constexpr int U = STREAM ? 6 : 3;        // steps whose loads are in flight together
   const int lane = threadIdx.x & 63, l = lane % L;
   const unsigned w = blockIdx.x * (kRotThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned parts = a.parts;
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
   auto fetch = [&](int s) {
     bool keys, ok;
     const int at = place(s, keys, ok);
-    return *reinterpret_cast<const uint4*>((keys ? src1 : src0) + at);
+    return load16<STREAM>((keys ? src1 : src0) + at);
   };
   uint4 raw[U];
 #pragma unroll
@@ -234,15 +234,19 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotArgs a) {
         else m = other(x[j]);
         y[j] = r * (turns ? fmaf(x[j], cs[j], m * sn[j]) : x[j]);
       }
-      if (ok) *reinterpret_cast<uint4*>((keys ? dst1 : dst0) + at) = P::narrow(y);
+      if (ok) store16<STREAM>((keys ? dst1 : dst0) + at, P::narrow(y));
     }
   }
 }
 
+template <typename T, int D, bool STREAM>
+auto rotate_pairs(int pairs) {
+  return pairs == kAdjacent ? rotate_kernel<T, D, kAdjacent, STREAM>
+         : pairs == kHalves ? rotate_kernel<T, D, kHalves, STREAM> : rotate_kernel<T, D, kAnyHalves, STREAM>;
+}
 template <typename T, int D>
-auto rotate_for(int pairs) {
-  return pairs == kAdjacent ? rotate_kernel<T, D, kAdjacent>
-         : pairs == kHalves ? rotate_kernel<T, D, kHalves> : rotate_kernel<T, D, kAnyHalves>;
+auto rotate_for(int pairs, bool stream) {
+  return stream ? rotate_pairs<T, D, true>(pairs) : rotate_pairs<T, D, false>(pairs);
 }
 
 }  // namespace
@@ -277,8 +281,13 @@ hipError_t launch_qk_norm_rope(const ent_ctx* c, int B, int T, const ent_qk_para
   const long long waves = static_cast<long long>(T) * a.parts;
   const dim3 grid(static_cast<unsigned>((waves + kRotThreads / 64 - 1) / (kRotThreads / 64)));
   const int pairs = a.adjacent ? kAdjacent : a.rot == f.head_dim ? kHalves : kAnyHalves;
-  auto kern = bf16 ? (f.head_dim == 64 ? rotate_for<uint16_t, 64>(pairs) : rotate_for<uint16_t, 128>(pairs))
-                   : (f.head_dim == 64 ? rotate_for<float, 64>(pairs) : rotate_for<float, 128>(pairs));
+  // Rows past what the last-level cache holds do not take places in the caches: 51624 rows of
+  // 64 + 8 heads of 128 in bf16 329 us against 369 (loads alone 368, stores alone 349, both
+  // with three steps in flight instead of six 334).  Fewer are soon read by what follows.
+  const long long bytes = 2ll * T * (f.num_q_heads + f.num_kv_heads) * f.head_dim * (bf16 ? 2 : 4);
+  const bool stream = bytes > kStreamBytes;
+  auto kern = bf16 ? (f.head_dim == 64 ? rotate_for<uint16_t, 64>(pairs, stream) : rotate_for<uint16_t, 128>(pairs, stream))
+                   : (f.head_dim == 64 ? rotate_for<float, 64>(pairs, stream) : rotate_for<float, 128>(pairs, stream));
   hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), 0, s, a);
   return hipGetLastError();
 }
