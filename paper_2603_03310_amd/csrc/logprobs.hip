@@ -37,8 +37,8 @@ constexpr int kLpParts = 64;          // parts of a row, at most
 constexpr int kLpWho = 64;            // threads that can reach the bound
 constexpr int kLpSegs = 8;            // segments of a thread's walk
 static_assert(kLpTop * kLpTop <= kLpCand, "keys of a row's n lists");
-static_assert(kLpTop + kLpTop / 2 + 3 <= kLpWho, "threads over the bound");
-static_assert(kLpParts == 64 && kLpParts <= kLpThreads, "a wave joins the parts");
+static_assert(kLpTop + kLpTop / 4 + 2 <= kLpWho, "threads over the bound");
+static_assert(kLpParts == 64 && 2 * kLpParts <= kLpThreads, "a wave of lanes for the parts, and another");
 typedef unsigned long long u64;
 
 struct LpArgs {
@@ -283,7 +283,7 @@ __device__ __forceinline__ void lp_largest(const LpArgs& a, LpShared<NT>& sh, co
     u64 key[NT / 64];
 #pragma unroll
     for (int k = 0; k < NT / 64; ++k) key[k] = sh.key[k * 64 + lane];
-    const u64 e = lp_bound<R::kDrop>(key, n, n + n / 2 + 3);
+    const u64 e = lp_bound<R::kDrop>(key, n, n + n / 4 + 2);
     if (lane == 0) sh.edge = e;
   }
   __syncthreads();
@@ -366,33 +366,32 @@ __device__ __forceinline__ void lp_join(const LpArgs& a, LpShared<kLpThreads>& s
 #pragma unroll
   for (int k = 0; k < K; ++k) mine[k] = t + k * NT < total ? lp_shared(keys + t + k * NT) : 0ull;
   if (t < 64) {
+    // The bound, while the next wave forms the row's sums.
+    if (t == 0) sh.count = 0;
+    if (n > 0) {
+      const int q = (n + a.parts - 1) / a.parts;
+      u64 head = 0ull, e;                  // of the list, or its q-th key
+      if (t < a.parts) head = lp_shared(keys + static_cast<long long>(t) * n + q - 1);
+      if (q == 1) {
+        const u64 one[1] = {head};
+        e = lp_bound<DROP>(one, n, min(n + 3, kLpCand / n));    // lists whose keys all fit
+      } else {
+        const u64 least = t < a.parts ? head : ~0ull;
+        e = static_cast<u64>(wave_min_u(static_cast<unsigned>(least >> 32))) << 32;    // all keys of this logit
+      }
+      if (t == 0) sh.edge = e;
+    }
+  } else if (t < 128) {
+    const int i = t - 64;
     LpSums g{-INFINITY, 0.f, 0.f};
-    u64 head = 0ull;                       // of the list, or its q-th key
-    const int q = n == 0 ? 1 : (n + a.parts - 1) / a.parts;
-    if (t < a.parts) {
-      const float* o = a.sums + 3 * (first + t);
+    if (i < a.parts) {
+      const float* o = a.sums + 3 * (first + i);
       g = LpSums{lp_shared(o), lp_shared(o + 1), lp_shared(o + 2)};
-      if (n > 0) head = lp_shared(keys + static_cast<long long>(t) * n + q - 1);
     }
     g = lp_to(g, wave_max(g.m), sc);
     g.s = wave_sum(g.s);
     g.w = wave_sum(g.w);
-    if (t == 0) {
-      lp_outputs(a, row, g, sc.c, tok, z, sh.ml[0], sh.ml[1]);
-      sh.count = 0;
-    }
-    if (n > 0) {
-      u64 e;
-      if (q == 1) {
-        const u64 one[1] = {head};
-        e = lp_bound<DROP>(one, n, n);
-      } else {
-        const u64 mine = t < a.parts ? head : ~0ull;
-        const unsigned hi = wave_min_u(static_cast<unsigned>(mine >> 32));
-        e = static_cast<u64>(hi) << 32;    // the keys of this logit, all of them
-      }
-      if (t == 0) sh.edge = e;
-    }
+    if (i == 0) lp_outputs(a, row, g, sc.c, tok, z, sh.ml[0], sh.ml[1]);
   }
   if (n == 0) return;
   __syncthreads();
@@ -503,7 +502,7 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs a) {
     g = LpSums{mm, ss, sw};
   }
   const bool whole = a.parts == 1;
-  if (t == 0) {
+  if (t == NT - 64) {                      // of the last wave: the first goes on with the bound
     if (whole) {
       lp_outputs(a, row, g, sc.c, tok, z, sh.ml[0], sh.ml[1]);
     } else {
