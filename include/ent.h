@@ -487,8 +487,8 @@ int ent_qk_norm_rope(ent_ctx* c, int B, int T, const ent_qk_params* prm, const v
  * arrays ([T, n_top]) unless n_top is 0.  Logits of -inf have probability 0.  A row
  * with a NaN or +inf, or with nothing but -inf, has no distribution: its outputs are
  * NaN and its ids -1.  Sums in 32 bits.  0 <= n_top <= min(vocab,
- * ENT_MAX_TOP_LOGPROBS); at most ENT_MAX_PACKED_TOKENS rows.  Only the context's
- * vocab and t_cal matter. */
+ * ENT_MAX_TOP_LOGPROBS); at most ENT_MAX_PACKED_TOKENS rows.  Outputs must not alias
+ * each other or an input.  Only the context's vocab and t_cal matter. */
 #define ENT_MAX_TOP_LOGPROBS 32
 int ent_token_logprobs(ent_ctx* c, int T, const void* logits, int logits_dtype, long long ld,
                        const int* tokens, const float* temp, float* logprob, float* entropy,

@@ -730,6 +730,12 @@ int ent_token_logprobs(ent_ctx* c, int T, const void* logits, int logits_dtype, 
     return fail(c, ENT_E_INVAL, "ent_token_logprobs: NULL required pointer");
   if (!aligned(logits, logits_dtype == ENT_BF16 ? 2 : 4))
     return fail(c, ENT_E_INVAL, "ent_token_logprobs: logits misaligned");
+  const void* outs[4] = {logprob, entropy, n_top > 0 ? top_ids : nullptr, n_top > 0 ? top_logprobs : nullptr};
+  for (int i = 0; i < 4; ++i) {
+    bool twice = outs[i] && (outs[i] == logits || outs[i] == tokens || outs[i] == temp);
+    for (int k = 0; k < i; ++k) twice = twice || (outs[i] && outs[i] == outs[k]);
+    if (twice) return fail(c, ENT_E_INVAL, "ent_token_logprobs: an output aliases another array");
+  }
   const hipError_t e = ent::launch_token_logprobs(c, T, logits, logits_dtype, ld, tokens, temp, logprob,
                                                   entropy, n_top, top_ids, top_logprobs,
                                                   static_cast<hipStream_t>(stream));
@@ -747,6 +753,8 @@ int ent_cache_fork(ent_ctx* c, int N, int R, const int* src, const int* dst, int
   if (N == 0) return ENT_OK;
   if (!src || !dst || !block_tables || !ctx_lens || !shared || (!free_ids && n_ids > 0) || !free_range)
     return fail(c, ENT_E_INVAL, "ent_cache_fork: NULL required pointer");
+  if (src == ctx_lens || dst == ctx_lens || shared == ctx_lens)
+    return fail(c, ENT_E_INVAL, "ent_cache_fork: ctx_lens aliases another array");
   if (int r = check_pages(c, "ent_cache_fork", k_cache, v_cache, k_scale, v_scale, ksum)) return r;
   const hipError_t e = ent::launch_cache_fork(c, N, R, src, dst, block_tables, ctx_lens, shared, free_ids,
                                               n_ids, free_range, k_cache, v_cache, k_scale, v_scale, ksum,
@@ -764,6 +772,8 @@ int ent_cache_release(ent_ctx* c, int N, int R, const int* rows, const int* bloc
   if (N == 0) return ENT_OK;
   if (!rows || !block_tables || !ctx_lens || (!free_ids && n_ids > 0) || !free_range)
     return fail(c, ENT_E_INVAL, "ent_cache_release: NULL required pointer");
+  if (rows == ctx_lens || shared == ctx_lens || rows == free_ids)
+    return fail(c, ENT_E_INVAL, "ent_cache_release: rows, ctx_lens, shared or free_ids alias each other");
   const hipError_t e = ent::launch_cache_release(c, N, R, rows, block_tables, ctx_lens, shared, free_ids,
                                                  n_ids, free_range, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(c, e, "ent_cache_release launch");

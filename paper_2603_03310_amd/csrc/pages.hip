@@ -61,7 +61,8 @@ __device__ __forceinline__ void copy_units(const uint4* __restrict__ s, uint4* _
 // Block `from`'s contents to block `to` by threads t of nt: two pieces of keys and two of
 // values in flight a thread.
 __device__ __forceinline__ void copy_block(const PageStore& st, int from, int to, int t, int nt) {
-  const uint4 *sk = at16(static_cast<const void*>(st.k), from * st.tile_bytes), *sv = at16(static_cast<const void*>(st.v), from * st.tile_bytes);
+  const uint4* sk = at16(static_cast<const void*>(st.k), from * st.tile_bytes);
+  const uint4* sv = at16(static_cast<const void*>(st.v), from * st.tile_bytes);
   uint4 *dk = at16(st.k, to * st.tile_bytes), *dv = at16(st.v, to * st.tile_bytes);
   const int units = static_cast<int>(st.tile_bytes / 16);
   int i = t;
@@ -79,7 +80,7 @@ __device__ __forceinline__ void copy_block(const PageStore& st, int from, int to
   }
   if (st.ksum)
     copy_units<1, false>(at16(static_cast<const void*>(st.ksum), 4ll * from * st.sum_floats),
-                  at16(st.ksum, 4ll * to * st.sum_floats), st.sum_floats / 4, t, nt);
+                         at16(st.ksum, 4ll * to * st.sum_floats), st.sum_floats / 4, t, nt);
   if (st.ks) {
     for (int i = t; i < st.Hkv; i += nt) {
       st.ks[static_cast<long long>(to) * st.Hkv + i] = st.ks[static_cast<long long>(from) * st.Hkv + i];
@@ -360,7 +361,7 @@ __global__ __launch_bounds__(kPageThreads) void fork_kernel(ForkArgs a) {
 // Release.  Every workgroup takes a holder from some of its sequence's blocks; a block
 // that had none left over keeps its count of 0 and goes into a bitmap.  The last
 // workgroup lists the bitmap and clears it.  Bound by the chain of round trips (row,
-// length, entry, count, bit, workgroup count, bitmap: one sequence of 8144 tokens 6.6 us)
+// length, entry, count, bit, workgroup count, bitmap: one sequence of 8144 tokens 7.0 us)
 // and by the last workgroup's instructions (112 sequences of 73368 entries, 13128 blocks
 // that become free: 14.2 us, 3.6 of them the list; with the list in a launch of one
 // workgroup and a thread per word 24).

@@ -219,12 +219,20 @@ def test_refusals(torch_cuda):
                 ent.ent_token_logprobs(dec.ctx, a["T"], a["z"], a["kind"], a["ld"], a["tk"], None, lp, None,
                                        a["n"], a["ids"], top)
             assert e.value.code == code, (kw, str(e.value))
+        h = torch.full((4,), -7.0, device="cuda:0")
+        for kw in (dict(entropy=lp), dict(temp=lp), dict(entropy=h, temp=h), dict(top_logprobs=lp), dict(top_ids=tk),
+                   dict(entropy=z), dict(top_ids=ids, top_logprobs=ids)):
+            a = dict(dict(entropy=None, temp=None, top_ids=ids, top_logprobs=top), **kw)
+            with pytest.raises(ent.EntError) as e:
+                ent.ent_token_logprobs(dec.ctx, 4, z, 0, 50, tk, a["temp"], lp, a["entropy"], 1, a["top_ids"],
+                                       a["top_logprobs"])
+            assert e.value.code == inval and "aliases" in str(e.value), kw
         with pytest.raises(ent.EntError):
             dec.logprobs(z.double(), tk, lp)
         with pytest.raises(ent.EntError):
             dec.logprobs(z.t().contiguous().t(), tk, lp)
         torch.cuda.synchronize()
-        assert (lp == -7.0).all().item()
+        assert (lp == -7.0).all().item() and (h == -7.0).all().item()
 
 
 def test_offsets_past_32_bits(torch_cuda):

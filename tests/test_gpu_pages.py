@@ -326,6 +326,10 @@ def test_refusals(torch_cuda):
                        dict(k=k.data_ptr() + 8), dict(ksum=ksum.data_ptr() + 4)):
                 refused(dec, inval, what, **kw)
         refused(dec, inval, "fork", dst=None)
+        for what, kw in (("fork", dict(rows=d["ctx"])), ("fork", dict(dst=d["ctx"])), ("fork", dict(shared=d["ctx"])),
+                         ("release", dict(rows=d["ctx"])), ("release", dict(shared=d["ctx"])),
+                         ("release", dict(rows=d["ids"]))):
+            refused(dec, inval, what, **kw)
         refused(dec, inval, "fork", shared=None)
         refused(dec, inval, "compact", n_ids=39)
         ent.ent_cache_fork(dec.ctx, 0, 4, *[None] * 6, 0, *[None] * 6)
