@@ -29,6 +29,7 @@ constexpr int kRotThreads = 256;
 // 8192 / 16384: 512 rows 7.6 / 7.8 / 9.7 / 10.0, 1024 rows 11.6 / 11.1 / 12.1 / 15.6, 2048
 // rows 18.2 / 15.3 / 17.0 / 18.6, 4096 rows 34.5 / 34.8 / 35.2 / 32.6.
 constexpr int kRotWaves = 4096;
+constexpr long long kRotStream = 160ll << 20;
 
 struct RotArgs {
   const void* src[2];     // queries, keys
@@ -281,11 +282,13 @@ hipError_t launch_qk_norm_rope(const ent_ctx* c, int B, int T, const ent_qk_para
   const long long waves = static_cast<long long>(T) * a.parts;
   const dim3 grid(static_cast<unsigned>((waves + kRotThreads / 64 - 1) / (kRotThreads / 64)));
   const int pairs = a.adjacent ? kAdjacent : a.rot == f.head_dim ? kHalves : kAnyHalves;
-  // Rows past what the last-level cache holds do not take places in the caches: 51624 rows of
-  // 64 + 8 heads of 128 in bf16 329 us against 369 (loads alone 368, stores alone 349, both
-  // with three steps in flight instead of six 334).  Fewer are soon read by what follows.
+  // Rows that leave the last-level cache little room for anything else take no places in the
+  // caches: 51624 rows of 64 + 8 heads of 128 in bf16 (1.9 GB) 329 us against 369 (loads alone
+  // 368, stores alone 349, both with three steps in flight instead of six 334), 184 MB 36.8
+  // against 43.1, 147 MB 31.1 against 32.7, 123 MB (of 40 heads) 26.5 against 24.8.  Fewer are
+  // soon read by what follows.
   const long long bytes = 2ll * T * (f.num_q_heads + f.num_kv_heads) * f.head_dim * (bf16 ? 2 : 4);
-  const bool stream = bytes > kStreamBytes;
+  const bool stream = bytes > kRotStream;
   auto kern = bf16 ? (f.head_dim == 64 ? rotate_for<uint16_t, 64>(pairs, stream) : rotate_for<uint16_t, 128>(pairs, stream))
                    : (f.head_dim == 64 ? rotate_for<float, 64>(pairs, stream) : rotate_for<float, 128>(pairs, stream));
   hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), 0, s, a);
