@@ -562,9 +562,9 @@ hipError_t launch_token_logprobs(const ent_ctx* c, int T, const void* logits, in
   const long long bytes = static_cast<long long>(a.V) * (bf16 ? 2 : 4);
   const int part16 = static_cast<int>((bytes + 16383) / 16384);
   a.parts = std::max(1, std::min({kLpParts, kLpSlots / T, std::max(std::min(c->num_cu / T, part16), (part16 + 1) / 2)}));
-  // Logits past what the last-level cache holds are read without a place in the caches: 2500
-  // rows of 128256 floats 238 us against 257 with (202 with 8 pieces of a thread in flight and
-  // steps without tests); 64 rows of bf16 18.8 against 18.4.
+  // Logits that fill the last-level cache are read without a place in the caches, and with 8
+  // pieces of a thread in flight: 2500 rows of 128256 floats 238 us against 257 (202 since), 512
+  // rows (263 MB) 51.6 against 53.7, 400 rows (205 MB) 47.8 against 47.2, 256 rows 30.5 / 28.7.
   const bool stream = bytes * T > kStreamBytes;
   // Short rows, and many of some length, to a wave each instead of to four: what a row
   // costs besides its reads is then four times as cheap, and rows are enough to fill the

@@ -666,7 +666,7 @@ hipError_t launch_cache_compact(const ent_ctx* c, int R, int* tables, const int*
   // Blocks of pools past the last-level cache take no places in the caches.  Us with / without,
   // 30% of a pool's blocks moved: 345 MB 42.1 / 40.8 (8-bit) and 39.1 / 36.5 (fp32), 430 MB
   // 50.1 / 53.3, 690 MB 64.5 / 71.1; 1.3 GB 137 / 154.
-  const bool stream = 2 * a.st.tile_bytes * c->cfg.num_pool_blocks > 3 * kStreamBytes / 2;
+  const bool stream = 2 * a.st.tile_bytes * c->cfg.num_pool_blocks > 2 * kStreamBytes;
   auto kern = stream ? compact_kernel<true> : compact_kernel<false>;
   hipLaunchKernelGGL(kern, dim3(a.row_wgs + copiers), dim3(kPageThreads), 0, s, a);
   return hipGetLastError();
