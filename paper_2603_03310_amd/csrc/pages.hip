@@ -18,8 +18,8 @@ namespace {
 
 constexpr int kPageThreads = 256;
 constexpr int kPlanThreads = 1024;
-// Bits of a word, on average, from which on a wave writes them together.  Always so: 10.0
-// us instead of 7.2 where 321 words have 509; from 32 on: 160 us instead of 158 for the
+// Bits of a word, on average, from which on a wave writes them together.  Always so: 9.2
+// us instead of 6.6 where 321 words have 509; from 32 on: 160 us instead of 158 for the
 // lists of 5120 moves over 320 words.
 constexpr int kDense = 8;
 constexpr int kBitPitch = kPageBitBytes / 8;     // 64-bit words from one word of a bitmap to the next
@@ -175,17 +175,25 @@ __device__ __forceinline__ void each_word(u64 b, int v, int n, u64* s_b, int* s_
 
 // Writes the ids of a workgroup's words (word t of thread t, of ids from id0 on; at most n
 // words with bits), the first of a thread's at `at` and so on; those before place 0 are
-// left out.  Where a word has few bits, each thread writes its own.
+// left out.  Where a word has few bits, each thread writes its own.  zero (nullable):
+// becomes 0 at each of the ids.
 template <int NT>
-__device__ __forceinline__ void list_bits(u64 b, int at, int id0, int n, bool dense, int* out, u64* s_b, int* s_v) {
+__device__ __forceinline__ void list_bits(u64 b, int at, int id0, int n, bool dense, int* out, u64* s_b, int* s_v,
+                                          int* zero) {
   if (dense) {
     each_word<NT>(b, at, n, s_b, s_v, [&](u64 w, int first, int i) {
-      const int place = first + bits_below(w);
-      if (bit_here(w) && place >= 0) out[place] = id0 + i * 64 + static_cast<int>(threadIdx.x & 63);
+      const int place = first + bits_below(w), id = id0 + i * 64 + static_cast<int>(threadIdx.x & 63);
+      if (bit_here(w)) {
+        if (place >= 0) out[place] = id;
+        if (zero) zero[id] = 0;
+      }
     });
   } else {
-    for (; b; b &= b - 1, ++at)
-      if (at >= 0) out[at] = id0 + static_cast<int>(threadIdx.x) * 64 + __builtin_ctzll(b);
+    for (; b; b &= b - 1, ++at) {
+      const int id = id0 + static_cast<int>(threadIdx.x) * 64 + __builtin_ctzll(b);
+      if (at >= 0) out[at] = id;
+      if (zero) zero[id] = 0;
+    }
   }
 }
 
@@ -359,12 +367,13 @@ __global__ __launch_bounds__(kPageThreads) void fork_kernel(ForkArgs a) {
 
 // ---------------------------------------------------------------------------
 // Release.  Every workgroup takes a holder from some of its sequence's blocks; a block
-// that had none left over keeps its count of 0 and goes into a bitmap.  The last
-// workgroup lists the bitmap and clears it.  Bound by the chain of round trips (row,
-// length, entry, count, bit, workgroup count, bitmap: one sequence of 8144 tokens 7.0 us)
-// and by the last workgroup's instructions (112 sequences of 73368 entries, 13128 blocks
-// that become free: 14.2 us, 3.6 of them the list; with the list in a launch of one
-// workgroup and a thread per word 24).
+// that had none left over goes into a bitmap.  The last workgroup lists the bitmap, clears
+// it and sets the counts of its blocks back to 0 (given back by who found none left, at
+// once: one atomic more in the chain, 7.3 and 14.2 us; the count read before it is taken
+// from: 6.2 and 21.3).  Bound by the chain of round trips (row, length, entry, count, bit,
+// workgroup count, bitmap: one sequence of 8144 tokens 6.6 us) and by the last workgroup's
+// instructions (112 sequences of 73368 entries, 13128 blocks that become free: 13.3 us;
+// with the list in a launch of one workgroup and a thread per word 24).
 // ---------------------------------------------------------------------------
 struct ReleaseArgs {
   Tables tb;
@@ -403,15 +412,16 @@ __global__ __launch_bounds__(kPlanThreads) void release_kernel(ReleaseArgs a) {
   } else {
     const int nb = (n + kBlock - 1) / kBlock;
     const int* tab = a.tb.tables + static_cast<long long>(row) * a.tb.MAXB;
-    // Whoever finds no holder left gives the count back, so it ends at 0; who finds the
-    // bit set then is one too many.
     for (int j = part * NT + t; j < nb; j += a.parts * NT) {
       const int p = tab[j];
       if (p < 0 || p >= a.tb.P) {
         bad |= ENT_DEV_BAD_TABLE;
-      } else if (!a.shared || atomicSub(&a.shared[p], 1) <= 0) {
-        if (a.shared) atomicAdd(&a.shared[p], 1);
-        if (set_bit(a.bits, p)) bad |= ENT_DEV_BAD_TABLE;
+      } else if (a.shared) {
+        const int others = atomicSub(&a.shared[p], 1);
+        if (others <= 0) (void)set_bit(a.bits, p);
+        if (others < 0) bad |= ENT_DEV_BAD_TABLE;      // listed more often than held
+      } else if (set_bit(a.bits, p)) {
+        bad |= ENT_DEV_BAD_TABLE;
       }
     }
   }
@@ -435,7 +445,7 @@ __global__ __launch_bounds__(kPlanThreads) void release_kernel(ReleaseArgs a) {
   for (int w0 = 0; w0 < words; w0 += NT) {
     if (w0 > 0) x = take_word(a.bits, w0 + t, words);
     if (words > NT) k = scan_before<NT>(popc(x), all, s_red);
-    list_bits<NT>(x, at + k, w0 * 64, words - w0, total >= kDense * words, a.ids, s_b, s_v);
+    list_bits<NT>(x, at + k, w0 * 64, words - w0, total >= kDense * words, a.ids, s_b, s_v, a.shared);
     if (words > NT) at += all;
   }
   if (t == 0) {
@@ -532,8 +542,8 @@ __global__ __launch_bounds__(kPlanThreads) void mark_kernel(CompactArgs a) {
     // Bits of ids below U.
     const u64 low = w >= words || base >= U ? 0ull : base + 64 <= U ? ~0ull : (1ull << (U - base)) - 1ull;
     const bool dense = U - below >= kDense * words;
-    list_bits<NT>(~x & low, base - k, w0 * 64, words - w0, dense, a.to, s_b, s_v);
-    list_bits<NT>(x & ~low, k + popc(x & low) - below, w0 * 64, words - w0, dense, a.from, s_b, s_v);
+    list_bits<NT>(~x & low, base - k, w0 * 64, words - w0, dense, a.to, s_b, s_v, nullptr);
+    list_bits<NT>(x & ~low, k + popc(x & low) - below, w0 * 64, words - w0, dense, a.from, s_b, s_v, nullptr);
   }
   if (t == 0) {
     a.info[0] = U;
