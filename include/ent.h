@@ -505,13 +505,12 @@ int ent_token_logprobs(ent_ctx* c, int T, const void* logits, int logits_dtype, 
  * sequence is writing (not full) must be its own: forks copy that one and share the
  * full ones, which no call writes again.
  * Forks and releases with a free range outside [0, n_ids] change nothing
- * (ENT_DEV_BAD_TABLE).  A row out of [0, R) is passed over (ENT_DEV_BAD_ROW), a sequence whose length is out of
- * range too (ENT_DEV_BAD_CTXLEN); a table entry outside the pool is not followed
- * (ENT_DEV_BAD_TABLE).
+ * (ENT_DEV_BAD_TABLE).  A row out of [0, R) is passed over (ENT_DEV_BAD_ROW), a
+ * sequence whose length is out of range too (ENT_DEV_BAD_CTXLEN); a table entry
+ * outside the pool is not followed (ENT_DEV_BAD_TABLE).
  * k_cache, v_cache: of the context's type; ksum may be NULL in the exact scoring
- * mode; with k_scale and v_scale (both or
- * none) the caches hold 8-bit codes, as for the _q8 calls (same conditions).
- * Caches and ksum need 16-byte alignment. */
+ * mode; with k_scale and v_scale (both or none) the caches hold 8-bit codes, as for
+ * the _q8 calls (same conditions).  Caches and ksum need 16-byte alignment. */
 
 /* N forks: row dst[i] becomes a sequence like row src[i]'s, with its full blocks
  * shared and, where the last one is not full, a block of the free list with its
@@ -540,9 +539,9 @@ int ent_cache_release(ent_ctx* c, int N, int R, const int* rows, const int* bloc
 /* The U blocks that the R sequences hold move to the pool's lower end: each block
  * >= U among them, in ascending order, to the free places below U in ascending
  * order, with its keys, values, scales, mean keys and share count (nullable);
- * tables follow.  The free list, whatever it held, becomes U .. num_pool_blocks - 1 at the upper end
- * of free_ids (n_ids >= num_pool_blocks), and *n_used (device int, nullable) U.  A
- * block that none of the R sequences holds counts as free. */
+ * tables follow.  The free list, whatever it held, becomes U .. num_pool_blocks - 1
+ * at the upper end of free_ids (n_ids >= num_pool_blocks), and *n_used (device int,
+ * nullable) U.  A block that none of the R sequences holds counts as free. */
 int ent_cache_compact(ent_ctx* c, int R, int* block_tables, const int* ctx_lens, int* shared,
                       int* free_ids, int n_ids, int* free_range, void* k_cache, void* v_cache,
                       float* k_scale, float* v_scale, float* ksum, int* n_used, void* stream);
