@@ -538,10 +538,12 @@ int ent_cache_release(ent_ctx* c, int N, int R, const int* rows, const int* bloc
 
 /* The U blocks that the R sequences hold move to the pool's lower end: each block
  * >= U among them, in ascending order, to the free places below U in ascending
- * order, with its keys, values, scales, mean keys and share count (nullable);
- * tables follow.  The free list, whatever it held, becomes U .. num_pool_blocks - 1
- * at the upper end of free_ids (n_ids >= num_pool_blocks), and *n_used (device int,
- * nullable) U.  A block that none of the R sequences holds counts as free. */
+ * order, with its keys, values, scales and mean keys; tables follow.  The free list,
+ * whatever it held, becomes U .. num_pool_blocks - 1 at the upper end of free_ids
+ * (n_ids >= num_pool_blocks), and *n_used (device int, nullable) U.  A block that none
+ * of the R sequences holds counts as free.  shared (nullable), whatever it held, becomes
+ * for each block the entries of the R sequences that name it less one, and 0 for the
+ * free: also where sequences have gone without ent_cache_release. */
 int ent_cache_compact(ent_ctx* c, int R, int* block_tables, const int* ctx_lens, int* shared,
                       int* free_ids, int n_ids, int* free_range, void* k_cache, void* v_cache,
                       float* k_scale, float* v_scale, float* ksum, int* n_used, void* stream);

@@ -115,7 +115,7 @@ def release(rows, tables, ctx, shared, ids, free, P: int):
 def compact(tables, ctx, shared, ids, free, P: int, pools=()):
     """See ent_cache_compact: (flags, blocks in use)."""
     R, maxb = tables.shape
-    flags, used = 0, set()
+    flags, held = 0, {}
     rows = []
     for r in range(R):
         n = int(ctx[r])
@@ -126,16 +126,18 @@ def compact(tables, ctx, shared, ids, free, P: int, pools=()):
         for j in range(rows[-1][1]):
             p = int(tables[r, j])
             if 0 <= p < P:
-                used.add(p)
+                held[p] = held.get(p, 0) + 1
             else:
                 flags |= BAD_TABLE
-    U = len(used)
-    place = dict(zip(sorted(p for p in used if p >= U), (p for p in range(U) if p not in used)))
+    U = len(held)
+    place = dict(zip(sorted(p for p in held if p >= U), (p for p in range(U) if p not in held)))
     for a, b in place.items():
         for x in pools:
             x[b] = x[a]
-        if shared is not None:
-            shared[b], shared[a] = shared[a], 0
+    if shared is not None:
+        shared[:] = 0
+        for p, n in held.items():
+            shared[place.get(p, p)] = n - 1
     for r, nb in rows:
         for j in range(nb):
             tables[r, j] = place.get(int(tables[r, j]), tables[r, j])
