@@ -29,7 +29,8 @@
  *  - A context belongs to the HIP device current at ent_init; every call on it
  *    must be made with that device current (else ENT_E_INVAL, nothing
  *    launched).  ent_destroy accepts any current device.
- *  - Batch sizes: 0 <= B <= max_batch.  B == 0 launches nothing.
+ *  - Batch sizes: 0 <= B <= max_batch.  B == 0 launches nothing (but see
+ *    ent_cache_compact).
  *
  * Paged KV cache layout (block size 16 tokens, P = num_pool_blocks):
  *    k_cache [P, H_kv, 16, d]   token-major tile per (physical block, KV head)
@@ -543,7 +544,9 @@ int ent_cache_release(ent_ctx* c, int N, int R, const int* rows, const int* bloc
  * (n_ids >= num_pool_blocks), and *n_used (device int, nullable) U.  A block that none
  * of the R sequences holds counts as free.  shared (nullable), whatever it held, becomes
  * for each block the entries of the R sequences that name it less one, and 0 for the
- * free: also where sequences have gone without ent_cache_release. */
+ * free: also where sequences have gone without ent_cache_release.  With R 0 the whole
+ * pool is free (tables and lengths are not read and may be NULL); nothing is done if
+ * free_ids, free_range, shared and n_used are NULL then. */
 int ent_cache_compact(ent_ctx* c, int R, int* block_tables, const int* ctx_lens, int* shared,
                       int* free_ids, int n_ids, int* free_range, void* k_cache, void* v_cache,
                       float* k_scale, float* v_scale, float* ksum, int* n_used, void* stream);

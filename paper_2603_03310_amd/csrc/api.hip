@@ -788,8 +788,8 @@ int ent_cache_compact(ent_ctx* c, int R, int* block_tables, const int* ctx_lens,
   if (int r = check_sequences(c, "ent_cache_compact", 0, R, n_ids)) return r;
   if (n_ids < c->cfg.num_pool_blocks)
     return fail(c, ENT_E_INVAL, "ent_cache_compact: free_ids needs room for num_pool_blocks ids");
-  if (R == 0) return ENT_OK;
-  if (!block_tables || !ctx_lens || !free_ids || !free_range)
+  if (R == 0 && !free_ids && !free_range && !shared && !n_used) return ENT_OK;
+  if ((R > 0 && (!block_tables || !ctx_lens)) || !free_ids || !free_range)
     return fail(c, ENT_E_INVAL, "ent_cache_compact: NULL required pointer");
   if (int r = check_pages(c, "ent_cache_compact", k_cache, v_cache, k_scale, v_scale, ksum)) return r;
   const hipError_t e = ent::launch_cache_compact(c, R, block_tables, ctx_lens, shared, free_ids, n_ids,

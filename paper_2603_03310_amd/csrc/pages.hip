@@ -462,11 +462,11 @@ __global__ __launch_bounds__(kPlanThreads) void release_kernel(ReleaseArgs a) {
 // are in any order.  Share counts are formed anew (sequences may have gone without a
 // release): -1 for every block in the first launch, and in the second one more for each
 // entry at its block's new place, and 0 for the free (10.4 us with 53 moves as without;
-// 1004 sequences of 251 holders a block 237 us, 190 without).  Bound by the copies: 5120 moved blocks of 64 KB and
-// their mean keys (713 MB) in 126 us of 137 = 5.7 TB/s, over a large copy's 4.7; the first
-// launch's 11 are the chain of round trips and 5 for the lists of moves.  (One workgroup
-// for a block, keys before values, four pieces a thread: 196 us in all; through the caches
-// 157.)
+// 1004 sequences, 251 holders a block, 237 us, 190 without).  Bound by the copies: 5120
+// moved blocks of 64 KB and their mean keys (713 MB) in 126 us of 137 = 5.7 TB/s, over a
+// large copy's 4.7; the first launch's 11 are the chain of round trips and 5 for the lists
+// of moves.  (One workgroup for a block, keys before values, four pieces a thread: 196 us
+// in all; through the caches 157.)
 // ---------------------------------------------------------------------------
 struct CompactArgs {
   Tables tb;
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(kPlanThreads) void mark_kernel(CompactArgs a) {
   __shared__ int s_below, s_last;
   constexpr int NT = kPlanThreads;
   const int t = threadIdx.x, row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-  const int n = a.tb.ctx[row];
+  const int n = row < a.tb.R ? a.tb.ctx[row] : 0;      // without sequences: one workgroup that marks nothing
   unsigned bad = 0;
   if (n < 0 || n > a.tb.MAXB * kBlock) {
     bad = ENT_DEV_BAD_CTXLEN;
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(kPageThreads) void compact_kernel(CompactArgs a) {
   }
   if (moves == 0 && !a.shared) return;
   const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-  const int n = a.tb.ctx[row];
+  const int n = row < a.tb.R ? a.tb.ctx[row] : 0;
   if (n < 0 || n > a.tb.MAXB * kBlock) return;
   const int nb = (n + kBlock - 1) / kBlock;
   int* tab = a.tb.tables + static_cast<long long>(row) * a.tb.MAXB;
@@ -667,15 +667,16 @@ hipError_t launch_cache_compact(const ent_ctx* c, int R, int* tables, const int*
                                 int* free_ids, int n_ids, int* free_range, void* k_cache,
                                 void* v_cache, float* k_scale, float* v_scale, float* ksum,
                                 int* n_used, hipStream_t s) {
+  const int rows = std::max(R, 1);
   CompactArgs a{page_tables(c, R, tables, const_cast<int*>(ctx_lens)), shared, free_ids, n_ids, free_range,
                 n_used, c->page_bits, c->page_words, c->page_sums, c->kept_phys,
                 reinterpret_cast<int*>(c->iscores), c->page_info, c->tickets,
-                row_parts(c, R, kPlanThreads), 0, page_store(c, k_cache, v_cache, k_scale, v_scale, ksum)};
-  hipLaunchKernelGGL(mark_kernel, dim3(R * a.parts), dim3(kPlanThreads), 0, s, a);
+                row_parts(c, rows, kPlanThreads), 0, page_store(c, k_cache, v_cache, k_scale, v_scale, ksum)};
+  hipLaunchKernelGGL(mark_kernel, dim3(rows * a.parts), dim3(kPlanThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  a.parts = row_parts(c, R, kPageThreads);
-  a.row_wgs = R * a.parts;
+  a.parts = row_parts(c, rows, kPageThreads);
+  a.row_wgs = rows * a.parts;
   // A workgroup for each half of a move, as far as the pool could have as many, up to 32 a CU
   // (5120 moves, us with 3 / 5 / 8 / 16 / 32 a CU: 142.5 / 143.9 / 145.5 / 140.7 / 137.4).
   const long long halves = std::min<long long>(c->cfg.num_pool_blocks, 2ll * R * c->cfg.max_blocks_per_seq);
