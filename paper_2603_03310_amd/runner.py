@@ -15,6 +15,13 @@ def make_config(**fields) -> ent.ent_config:
     return cfg
 
 
+def _need(name, x, dtype, n):
+    """x (None: left out) as the library takes it: n values at least, of this type, in one piece."""
+    if x is not None and not (x.dtype is dtype and x.numel() >= n and x.is_contiguous()):
+        raise ent.EntError(ent.ENT_E_INVAL, f"{name}: {x.dtype} {tuple(x.shape)} with strides {x.stride()}: "
+                                            f"{n} of {dtype} needed, in one piece")
+
+
 class Decoder:
     """Owns one library context; `step` runs the whole decode step, either as
     ent_entropy_temperature -> ent_block_select -> ent_sparse_paged_decode ->
@@ -113,30 +120,64 @@ class Decoder:
         """Log probabilities of tokens [T] under logits [T, vocab] (float32 or bfloat16)."""
         import torch
         kinds = {torch.float32: ent.ENT_F32, torch.bfloat16: ent.ENT_BF16}
-        if logits.dtype not in kinds or logits.stride(1) != 1:
-            raise ent.EntError(ent.ENT_E_INVAL, "logits: float32 or bfloat16 rows in one piece needed")
-        n_top = 0 if top_ids is None else top_ids.shape[1]
-        ent.ent_token_logprobs(self.ctx, logits.shape[0], logits, kinds[logits.dtype], logits.stride(0),
+        V = self.cfg.vocab
+        if logits.dtype not in kinds or logits.dim() != 2 or logits.stride(1) != 1 or logits.shape[1] < V:
+            raise ent.EntError(ent.ENT_E_INVAL, f"logits: float32 or bfloat16 rows of {V} in one piece needed")
+        T = logits.shape[0]
+        n_top = 0 if top_ids is None else top_ids.shape[-1]
+        _need("tokens", tokens, torch.int32, T)
+        for name, x in (("logprob", logprob), ("entropy", entropy), ("temp", temp)):
+            _need(name, x, torch.float32, T)
+        if n_top:
+            _need("top_ids", top_ids, torch.int32, T * n_top)
+            _need("top_logprobs", top_logprobs, torch.float32, T * n_top)
+            if top_logprobs is not None and top_logprobs.shape[-1] != n_top:
+                raise ent.EntError(ent.ENT_E_INVAL, f"top_logprobs of {top_logprobs.shape[-1]} columns, top_ids of {n_top}")
+        ent.ent_token_logprobs(self.ctx, T, logits, kinds[logits.dtype], logits.stride(0),
                                tokens, temp, logprob, entropy, n_top, top_ids, top_logprobs, stream)
 
     def fork(self, src, dst, block_tables, ctx_lens, shared, free_ids, free_range, k_cache, v_cache, ksum,
              k_scale=None, v_scale=None, stream=None):
         """Rows dst become sequences like rows src, whose full blocks they share."""
-        ent.ent_cache_fork(self.ctx, src.numel(), ctx_lens.numel(), src, dst, block_tables, ctx_lens, shared,
+        import torch
+        N = src.numel()
+        _need("src", src, torch.int32, N)
+        _need("dst", dst, torch.int32, N)
+        if dst.numel() != N:
+            raise ent.EntError(ent.ENT_E_INVAL, f"{dst.numel()} rows dst for {N} rows src")
+        self._sequences(block_tables, ctx_lens, shared, free_ids, free_range)
+        ent.ent_cache_fork(self.ctx, N, ctx_lens.numel(), src, dst, block_tables, ctx_lens, shared,
                            free_ids, free_ids.numel(), free_range, k_cache, v_cache, k_scale, v_scale, ksum,
                            stream)
 
     def release(self, rows, block_tables, ctx_lens, free_ids, free_range, shared=None, stream=None):
         """The sequences of these rows end; blocks that nobody holds go back to the free list."""
+        import torch
+        _need("rows", rows, torch.int32, rows.numel())
+        self._sequences(block_tables, ctx_lens, shared, free_ids, free_range)
         ent.ent_cache_release(self.ctx, rows.numel(), ctx_lens.numel(), rows, block_tables, ctx_lens, shared,
                               free_ids, free_ids.numel(), free_range, stream)
 
     def compact(self, block_tables, ctx_lens, free_ids, free_range, k_cache, v_cache, ksum, shared=None,
                 k_scale=None, v_scale=None, n_used=None, stream=None):
         """All blocks in use to the pool's lower end."""
+        import torch
+        self._sequences(block_tables, ctx_lens, shared, free_ids, free_range)
+        _need("n_used", n_used, torch.int32, 1)
         ent.ent_cache_compact(self.ctx, ctx_lens.numel(), block_tables, ctx_lens, shared, free_ids,
                               free_ids.numel(), free_range, k_cache, v_cache, k_scale, v_scale, ksum, n_used,
                               stream)
+
+    def _sequences(self, block_tables, ctx_lens, shared, free_ids, free_range):
+        import torch
+        R, width, i32 = ctx_lens.numel(), self.cfg.max_blocks_per_seq, torch.int32
+        _need("block_tables", block_tables, i32, R * width)
+        if block_tables.dim() != 2 or block_tables.shape[1] != width:
+            raise ent.EntError(ent.ENT_E_INVAL, f"block_tables {tuple(block_tables.shape)}: [{R}, {width}] needed")
+        _need("ctx_lens", ctx_lens, i32, R)
+        _need("shared", shared, i32, self.cfg.num_pool_blocks)
+        _need("free_ids", free_ids, i32, 0)
+        _need("free_range", free_range, i32, 2)
 
     def _rows(self, x, T, heads):
         """The row stride of T packed rows of whole heads, side by side."""
