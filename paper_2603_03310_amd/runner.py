@@ -110,7 +110,13 @@ class Decoder:
     def rotate(self, B, prm, q, k, q_out, k_out, starts=None, ctx_lens=None, stream=None):
         """Norms and rotation of rows q, q_out [T, H_q, d] and k, k_out [T, H_kv, d] (outputs may be
         the inputs); without starts, row b is sequence b's next token."""
+        import torch
         T, Hq, Hkv = q.shape[0], self.cfg.num_q_heads, self.cfg.num_kv_heads
+        _need("starts", starts, torch.int32, B + 1)
+        _need("ctx_lens", ctx_lens, torch.int32, B)
+        for name, x, n in zip(("q_gain", "k_gain", "inv_freq"), getattr(prm, "tensors", ()),
+                              (self.cfg.head_dim, self.cfg.head_dim, prm.rot_dim // 2)):
+            _need(name, x, torch.float32, n)
         ldq, ldk, ldqo, ldko = (self._rows(x, T, H) for x, H in ((q, Hq), (k, Hkv), (q_out, Hq), (k_out, Hkv)))
         ent.ent_qk_norm_rope(self.ctx, B, T, prm, q, ldq, k, ldk, starts, ctx_lens, q_out, ldqo, k_out,
                              ldko, stream)

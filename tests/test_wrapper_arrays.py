@@ -1,4 +1,4 @@
-"""Decoder.fork, release, compact and logprobs refuse arrays that the library would read or
+"""Decoder.fork, release, compact, logprobs and rotate refuse arrays that the library would read or
 write past their end, or take for another type; larger ones, as a program keeps them, do.  The
 library itself is not called."""
 import pytest
@@ -13,8 +13,9 @@ P, R, MAXB, V, T = 40, 4, 5, 50, 6
 @pytest.fixture
 def dec(monkeypatch):
     d = Decoder.__new__(Decoder)
-    d.cfg, d.ctx, d.calls = make_config(max_batch=8, max_blocks_per_seq=MAXB, num_pool_blocks=P, vocab=V), None, []
-    for name in ("ent_cache_fork", "ent_cache_release", "ent_cache_compact", "ent_token_logprobs"):
+    d.cfg, d.ctx, d.calls = make_config(max_batch=8, num_q_heads=4, num_kv_heads=2, head_dim=64, max_blocks_per_seq=MAXB, num_pool_blocks=P, vocab=V), None, []
+    for name in ("ent_cache_fork", "ent_cache_release", "ent_cache_compact", "ent_token_logprobs",
+                 "ent_qk_norm_rope"):
         monkeypatch.setattr(ent, name, lambda *a, n=name: d.calls.append((n, a)))
     return d
 
@@ -98,3 +99,29 @@ def test_logprobs_pass_arrays_on(dec):
     dec.logprobs(**rows(tokens=None, logprob=None, temp=None, top_ids=None, top_logprobs=None))
     assert [c[1][1] for c in dec.calls] == [T] * 3 and dec.calls[1][1][4] == V + 7
     assert [c[1][9] for c in dec.calls] == [3, 3, 0]
+
+
+def turned(starts=ints(4), ctx_lens=ints(3), gains=(torch.ones(64), torch.ones(64)), freq=torch.ones(16), B=3):
+    q, k = torch.zeros(T, 4, 64), torch.zeros(T, 2, 64)
+    return (B, ent.make_qk_params(*gains, freq, 1e-6, 32), q, k, q, k), dict(starts=starts, ctx_lens=ctx_lens)
+
+
+@pytest.mark.parametrize("name,kw", [
+    ("starts", dict(starts=ints(3))), ("starts", dict(starts=ints(4).to(LONG))), ("starts", dict(starts=ints(8)[::2])),
+    ("ctx_lens", dict(ctx_lens=ints(2))), ("ctx_lens", dict(ctx_lens=ints(3).to(LONG))),
+    ("q_gain", dict(gains=(torch.ones(63), None))), ("q_gain", dict(gains=(torch.ones(64).bfloat16(), None))),
+    ("k_gain", dict(gains=(None, torch.ones(64).double()))), ("k_gain", dict(gains=(None, torch.ones(128)[::2]))),
+    ("inv_freq", dict(freq=torch.ones(15))), ("inv_freq", dict(freq=torch.ones(16).double()))], ids=lambda v: v if isinstance(v, str) else "")
+def test_rotate_refuses(dec, name, kw):
+    a, b = turned(**kw)
+    with pytest.raises(ent.EntError) as e:
+        dec.rotate(*a, **b)
+    assert e.value.code == ent.ENT_E_INVAL and name in str(e.value) and not dec.calls
+
+
+def test_rotate_passes_arrays_on(dec):
+    for kw in (dict(), dict(starts=ints(9), ctx_lens=ints(9)), dict(ctx_lens=None, gains=(None, None)),
+               dict(starts=ints(1), B=0), dict(starts=None, B=3), dict(freq=torch.ones(40))):
+        a, b = turned(**kw)
+        dec.rotate(*a, **b)
+    assert [c[1][1] for c in dec.calls] == [3, 3, 3, 0, 3, 3]
