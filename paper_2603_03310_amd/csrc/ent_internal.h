@@ -18,7 +18,10 @@ constexpr int kMinTickets = 1024;           // counters in the workspace, at lea
 constexpr int kMaxBlocksPerSeq = 16384;     // selection keeps all scores in LDS
 constexpr int kEstChunkThreads = 256;       // threads of an entropy chunk job (maxima per chunk)
 constexpr int kPageBitBytes = 64;           // from one word of the block bitmap to the next
-constexpr long long kStreamBytes = 208ll << 20;   // traffic that leaves the last-level cache (256 MB) no room
+// Traffic that leaves the last-level cache (256 MB) no room for anything else: bytes that
+// are read, and bytes read and written where as many are written.
+constexpr long long kStreamBytes = 208ll << 20;
+constexpr long long kStreamCopyBytes = 144ll << 20;
 constexpr int kLpSlots = 1024;              // parts of the rows that log probabilities are cut into
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;

@@ -43,7 +43,9 @@ __device__ __forceinline__ uint4* at16(void* p, long long byte) {
   return reinterpret_cast<uint4*>(static_cast<char*>(p) + byte);
 }
 
-// The copy of `units` 16-byte pieces by threads t of nt, U of a thread in flight.
+// The copy of `units` 16-byte pieces by threads t of nt: U of a thread in flight while each
+// has as many left (with 8 and 256 threads, blocks of 32 KB and their multiples), then one
+// after the other, each a round trip.
 template <int U, bool STREAM>
 __device__ __forceinline__ void copy_units(const uint4* __restrict__ s, uint4* __restrict__ d, int units, int t,
                                            int nt) {
@@ -560,28 +562,38 @@ __global__ __launch_bounds__(kPlanThreads) void mark_kernel(CompactArgs a) {
   }
 }
 
-// Workgroups [0, row_wgs) take rows of the tables and the free list, the others blocks:
-// one the keys and what belongs to them, one the values.
+// Half a move by a workgroup: the keys and what belongs to them, or the values.
 template <bool STREAM>
+__device__ __forceinline__ void move_half(const PageStore& st, int from, int to, bool keys) {
+  const int t = threadIdx.x;
+  char* const base = keys ? st.k : st.v;
+  copy_units<8, STREAM>(at16(static_cast<const void*>(base), from * st.tile_bytes), at16(base, to * st.tile_bytes),
+                        static_cast<int>(st.tile_bytes / 16), t, kPageThreads);
+  if (keys && st.ksum)
+    copy_units<1, STREAM>(at16(static_cast<const void*>(st.ksum), 4ll * from * st.sum_floats),
+                          at16(st.ksum, 4ll * to * st.sum_floats), st.sum_floats / 4, t, kPageThreads);
+  if (st.ks) {
+    float* sc = keys ? st.ks : st.vs;
+    for (int i = t; i < st.Hkv; i += kPageThreads)
+      sc[static_cast<long long>(to) * st.Hkv + i] = sc[static_cast<long long>(from) * st.Hkv + i];
+  }
+}
+
+// Workgroups [0, row_wgs) take rows of the tables and the free list, the others blocks.
 __global__ __launch_bounds__(kPageThreads) void compact_kernel(CompactArgs a) {
   const int U = a.info[0], below = a.info[1], moves = U - below;
   const int t = threadIdx.x;
   if (blockIdx.x >= static_cast<unsigned>(a.row_wgs)) {
-    const int units = static_cast<int>(a.st.tile_bytes / 16);
+    // By what is moved, not by the pool: few blocks of a large one are soon read again.  Us
+    // with / without places in the caches, MB read and written: blocks of 64 KB 27: 13.2 /
+    // 15.5, 67: 21.0 / 24.3, 134: 34.1 / 37.7, 174: 47.8 / 45.6, 268: 69.7 / 63.2, 671: 152 /
+    // 143; of 8-bit codes 134: 39.1 / 41.0, 168: 49.9 / 47.0; of 4 heads of 64 134: 39.4 / 40.3,
+    // 168: 48.5 / 46.3; of floats 134: 32.7 / 36.9, 174: 46.8 / 45.7.
+    const bool stream = 4 * a.st.tile_bytes * moves > kStreamCopyBytes;
     for (int m = blockIdx.x - a.row_wgs; m < 2 * moves; m += gridDim.x - a.row_wgs) {
       const int from = a.from[m >> 1], to = a.to[m >> 1];
-      const bool keys = (m & 1) == 0;
-      char* const base = keys ? a.st.k : a.st.v;
-      copy_units<8, STREAM>(at16(static_cast<const void*>(base), from * a.st.tile_bytes), at16(base, to * a.st.tile_bytes),
-                    units, t, kPageThreads);
-      if (keys && a.st.ksum)
-        copy_units<1, STREAM>(at16(static_cast<const void*>(a.st.ksum), 4ll * from * a.st.sum_floats),
-                      at16(a.st.ksum, 4ll * to * a.st.sum_floats), a.st.sum_floats / 4, t, kPageThreads);
-      if (a.st.ks) {
-        float* sc = keys ? a.st.ks : a.st.vs;
-        for (int i = t; i < a.st.Hkv; i += kPageThreads)
-          sc[static_cast<long long>(to) * a.st.Hkv + i] = sc[static_cast<long long>(from) * a.st.Hkv + i];
-      }
+      if (stream) move_half<true>(a.st, from, to, (m & 1) == 0);
+      else move_half<false>(a.st, from, to, (m & 1) == 0);
     }
     return;
   }
@@ -681,12 +693,7 @@ hipError_t launch_cache_compact(const ent_ctx* c, int R, int* tables, const int*
   // (5120 moves, us with 3 / 5 / 8 / 16 / 32 a CU: 142.5 / 143.9 / 145.5 / 140.7 / 137.4).
   const long long halves = std::min<long long>(c->cfg.num_pool_blocks, 2ll * R * c->cfg.max_blocks_per_seq);
   const int copiers = static_cast<int>(std::min<long long>(std::max(halves, 1ll), 32ll * c->num_cu));
-  // Blocks of pools past the last-level cache take no places in the caches.  Us with / without,
-  // 30% of a pool's blocks moved: 345 MB 42.1 / 40.8 (8-bit) and 39.1 / 36.5 (fp32), 430 MB
-  // 50.1 / 53.3, 690 MB 64.5 / 71.1; 1.3 GB 137 / 154.
-  const bool stream = 2 * a.st.tile_bytes * c->cfg.num_pool_blocks > 2 * kStreamBytes;
-  auto kern = stream ? compact_kernel<true> : compact_kernel<false>;
-  hipLaunchKernelGGL(kern, dim3(a.row_wgs + copiers), dim3(kPageThreads), 0, s, a);
+  hipLaunchKernelGGL(compact_kernel, dim3(a.row_wgs + copiers), dim3(kPageThreads), 0, s, a);
   return hipGetLastError();
 }
 
