@@ -29,7 +29,8 @@ constexpr int kRotThreads = 256;
 // 8192 / 16384: 512 rows 7.6 / 7.8 / 9.7 / 10.0, 1024 rows 11.6 / 11.1 / 12.1 / 15.6, 2048
 // rows 18.2 / 15.3 / 17.0 / 18.6, 4096 rows 34.5 / 34.8 / 35.2 / 32.6.
 constexpr int kRotWaves = 4096;
-constexpr long long kRotStream = 160ll << 20;
+// Steps of a wave from which on rows past the caches are streamed.
+constexpr int kRotStreamSteps = 4;
 
 struct RotArgs {
   const void* src[2];     // queries, keys
@@ -284,11 +285,14 @@ hipError_t launch_qk_norm_rope(const ent_ctx* c, int B, int T, const ent_qk_para
   const int pairs = a.adjacent ? kAdjacent : a.rot == f.head_dim ? kHalves : kAnyHalves;
   // Rows that leave the last-level cache little room for anything else take no places in the
   // caches: 51624 rows of 64 + 8 heads of 128 in bf16 (1.9 GB) 329 us against 369 (loads alone
-  // 368, stores alone 349, both with three steps in flight instead of six 334), 184 MB 36.8
-  // against 43.1, 147 MB 31.1 against 32.7, 123 MB (of 40 heads) 26.5 against 24.8.  Fewer are
-  // soon read by what follows.
+  // 368, stores alone 349, both with three steps in flight instead of six 334).  Fewer are soon
+  // read by what follows.  Us streamed / not, MB read and written: 64 + 8 heads of 128 123:
+  // 28.4 / 28.3, 147: 31.0 / 32.7, 184: 36.7 / 42.7; 16 + 8 of 128 123: 26.3 / 22.7, 147: 29.7 /
+  // 30.3, 180: 35.3 / 39.9; of floats, 32 + 8 of 64, 123: 22.9 / 24.5, 180: 35.0 / 44.0.  Rows of
+  // few steps load some pieces twice for want of six: 16 + 4 heads of 64 (3 steps) 184: 48.4 /
+  // 45.2, 400: 101 / 88; 8 + 8 of 128 (4) 180: 38.0 / 40.5, 300: 59.6 / 61.3, 1000: 188 / 186.
   const long long bytes = 2ll * T * (f.num_q_heads + f.num_kv_heads) * f.head_dim * (bf16 ? 2 : 4);
-  const bool stream = bytes > kRotStream;
+  const bool stream = bytes > kStreamCopyBytes && steps / a.parts >= kRotStreamSteps;
   auto kern = bf16 ? (f.head_dim == 64 ? rotate_for<uint16_t, 64>(pairs, stream) : rotate_for<uint16_t, 128>(pairs, stream))
                    : (f.head_dim == 64 ? rotate_for<float, 64>(pairs, stream) : rotate_for<float, 128>(pairs, stream));
   hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), 0, s, a);

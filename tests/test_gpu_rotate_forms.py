@@ -1,7 +1,7 @@
 """ent_qk_norm_rope where a wave takes all steps of a row (more than 4096 rows) and more of
 them than are in flight together, with the queries' gains and then the keys': every element
 type, head size and pairing, below and above the size from which on rows take no places in the
-caches (160 MB read and written), in place and apart.  Every row against the formula in 64 bits."""
+caches (some 150 MB read and written), in place and apart.  Every row against the formula in 64 bits."""
 import numpy as np
 import pytest
 
@@ -78,3 +78,28 @@ def test_rows_of_many_steps(torch_cuda, dtype, d, pairs, T, norms):
     assert torch.equal(rows[:, Hq + Hkv:], before[:, Hq + Hkv:])
     if not in_place:
         assert torch.equal(rows, before)
+
+
+@pytest.mark.parametrize("pairs", ["halves", "adjacent"])
+def test_large_rows_of_few_steps(torch_cuda, pairs):
+    """Three and four steps a row (16 + 4 heads of 64, 8 + 8 of 128), past the caches."""
+    torch = torch_cuda
+    from paper_2603_03310_amd.runner import Decoder
+    for Hq, Hkv, d in ((16, 4, 64), (8, 8, 128)):
+        rot, adjacent = PAIRS[pairs](d)
+        T = (180 * 10**6) // (4 * (Hq + Hkv) * d)
+        g = torch.Generator(device="cuda:0")
+        g.manual_seed(T)
+        q, k = (torch.empty((T, h, d), dtype=torch.bfloat16, device="cuda:0").normal_(generator=g) for h in (Hq, Hkv))
+        outs = tuple(torch.empty_like(x) for x in (q, k))
+        prm, gains = params(torch, np.random.default_rng(T), d, rot, adjacent, (1, 1))
+        starts = torch.tensor([0, T // 3, T], dtype=torch.int32, device="cuda:0")
+        with Decoder(**config(Hq, Hkv, d)) as dec:
+            dec.rotate(2, prm, q, k, *outs, starts=starts)
+            torch.cuda.synchronize()
+            assert dec.device_status() == 0
+        pos = torch.arange(T, device="cuda:0")
+        pos[T // 3:] -= T // 3
+        for got, x, gain in zip(outs, (q, k), gains):
+            ref, size = formula(torch, x, pos, gain, freqs(rot), 1e-5, rot, adjacent)
+            assert ((got.double() - ref).abs() <= 17 * U32 * size + BF16_HALF * ref.abs() + 1e-37).all().item()
