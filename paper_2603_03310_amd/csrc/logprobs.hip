@@ -555,16 +555,24 @@ hipError_t launch_token_logprobs(const ent_ctx* c, int T, const void* logits, in
   a.flags = c->dev_flags;
   const bool bf16 = logits_dtype == ENT_BF16;
   // Parts of a row.  A workgroup a CU, of 16 KB at least; where that leaves a part more
-  // than 32 KB, more of them, up to four a CU.  Us with 128 / 256 / 512 / 1024 workgroups
-  // (n_top 5, 128256 logits): 4 rows of floats 10.2 / 11.4, 16 rows 13.3 / 12.8 / 14.7,
-  // 64 rows - / 20.6 / 17.1 / 17.7, 64 of bf16 - / 17.2 / 17.1 / 18.8 (n_top 20: 18.1 /
-  // 15.7 / 17.9), 256 of bf16 - / 40 / 28 / 23.
+  // than 32 KB, two a CU, and where it is then more than 16384 logits, up to four.  Us with
+  // 128 / 256 / 512 / 1024 workgroups (n_top 5, 128256 logits): 4 rows of floats 9.6 / 10.7,
+  // 16 rows 12.0 / 11.9 / 14.4, 32 rows 15.8 / 12.7 / 13.3, 64 rows 22.2 / 16.6 / 15.0 / 17.6,
+  // 128 rows - / 22.9 / 19.0 / 19.4 (of 32000 - / 12.2 / 11.3), 256 rows - / 38 / 27.6 / 28.9; 16
+  // rows of bf16 11.3 / 11.8 / 14.8, 64 rows 17.8 / 13.4 / 13.1 / 15.6 (n_top 20: 18.4 / 14.3 /
+  // 14.3 / 17.8), 128 rows - / 18.8 / 16.7 / 16.5, 256 rows - / 24.5 / 22.7 / 21.9.  More rows than
+  // CUs in two parts / whole: 400 of floats 47.3 / 45.9, 512 51.6 / 47.4; of bf16, n_top 0, 26.8 /
+  // 27.6 and 27.3 / 30.0.
   const long long bytes = static_cast<long long>(a.V) * (bf16 ? 2 : 4);
   const int part16 = static_cast<int>((bytes + 16383) / 16384);
-  a.parts = std::max(1, std::min({kLpParts, kLpSlots / T, std::max(std::min(c->num_cu / T, part16), (part16 + 1) / 2)}));
+  const int longest = (a.V + 16383) / 16384, one = c->num_cu / T, two = 2 * c->num_cu / T;
+  a.parts = std::max(std::min(one, part16), std::min((part16 + 1) / 2, std::max(two, longest)));
+  a.parts = std::max(1, std::min({kLpParts, kLpSlots / T, a.parts}));
   // Logits that fill the last-level cache are read without a place in the caches, and with 8
-  // pieces of a thread in flight: 2500 rows of 128256 floats 238 us against 257 (202 since), 512
-  // rows (263 MB) 51.6 against 53.7, 400 rows (205 MB) 47.8 against 47.2, 256 rows 30.5 / 28.7.
+  // pieces of a thread in flight.  Us streamed / not (128256 logits, n_top 5): of floats
+  // 1 GB 166 / 186, 263 MB 51.4 / 53.6, 230 MB 48.9 / 49.0, 205 MB 47.4 / 47.1,
+  // 130 MB 30.4 / 28.4; of bf16 500 MB 91.0 / 99.6, 230 MB 50.4 / 51.8, 205 MB 49.0 / 50.4, 130 MB
+  // 35.4 / 32.3.
   const bool stream = bytes * T > kStreamBytes;
   // Short rows, and many of some length, to a wave each instead of to four: what a row
   // costs besides its reads is then four times as cheap, and rows are enough to fill the

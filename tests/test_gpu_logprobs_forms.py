@@ -1,5 +1,5 @@
 """ent_token_logprobs in the forms that large calls take: bf16 rows that are read without a
-place in the caches (more than 208 MB), and rows of some length to a wave each (2048 rows and
+place in the caches (more than 218 MB), and rows of some length to a wave each (2048 rows and
 more of up to 32 KB on 256 CUs), with ties, masks, rows without a distribution, unaligned rows,
 and more candidates than a wave ranks at once.  A sample of rows against the oracle."""
 import numpy as np
