@@ -791,6 +791,8 @@ int ent_cache_compact(ent_ctx* c, int R, int* block_tables, const int* ctx_lens,
   if (R == 0 && !free_ids && !free_range && !shared && !n_used) return ENT_OK;
   if ((R > 0 && (!block_tables || !ctx_lens)) || !free_ids || !free_range)
     return fail(c, ENT_E_INVAL, "ent_cache_compact: NULL required pointer");
+  if (shared && (shared == ctx_lens || shared == block_tables || shared == free_ids || shared == n_used))
+    return fail(c, ENT_E_INVAL, "ent_cache_compact: shared aliases another array");
   if (int r = check_pages(c, "ent_cache_compact", k_cache, v_cache, k_scale, v_scale, ksum)) return r;
   const hipError_t e = ent::launch_cache_compact(c, R, block_tables, ctx_lens, shared, free_ids, n_ids,
                                                  free_range, k_cache, v_cache, k_scale, v_scale, ksum,

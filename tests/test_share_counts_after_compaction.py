@@ -133,3 +133,21 @@ def test_in_a_graph(torch_cuda):
             torch.cuda.synchronize()
             p.same()
         assert dec.device_status() == 0
+
+
+@pytest.mark.gpu
+def test_counts_in_another_array(torch_cuda):
+    """Counts are written before tables and lengths are read again."""
+    from paper_2603_03310_amd import ent
+    p = Pool(torch_cuda, [20, 33], 4, 40, 4, seed=9)
+    p.upload()
+    d = p.d
+    k, v, ksum, _ = p.caches()
+    with decoder(p) as dec:
+        for name in ("ctx", "tables", "ids"):
+            with pytest.raises(ent.EntError) as e:
+                ent.ent_cache_compact(dec.ctx, 4, d["tables"], d["ctx"], d[name], d["ids"], 40, d["free"], k, v, None,
+                                      None, ksum)
+            assert e.value.code == ent.ENT_E_INVAL and "aliases" in str(e.value), name
+        torch_cuda.cuda.synchronize()
+        p.same()
