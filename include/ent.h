@@ -459,12 +459,13 @@ typedef struct {
  *                           w = pos * inv_freq[i]
  *   dims from rot_dim on stay y.
  * Sums in 32 bits, angles in 64 up to the reduction to one turn, outputs rounded
- * once to kv_dtype; squares must not overflow 32 bits.  Positions: with starts
- * (int [B + 1], as ent_prompt_plan gives them), row t of request b has position
- * ctx_lens[b] + t - starts[b], and rows that belong to no request are left as they
- * are; with starts NULL, T must be B and row b has position ctx_lens[b] (a decode
- * step's new tokens, before ent_kv_append counts them).  ctx_lens NULL: all 0.  A
- * request whose ctx_lens is out of range keeps its rows (ENT_DEV_BAD_CTXLEN).
+ * once to kv_dtype; squares must not overflow 32 bits, nor all vanish in them where
+ * eps is 0.  Positions: with starts (int [B + 1], as ent_prompt_plan gives them), row t
+ * of request b has position ctx_lens[b] + t - starts[b], and rows that belong to no
+ * request are left as they are; with starts NULL, T must be B and row b has position
+ * ctx_lens[b] (a decode step's new tokens, before ent_kv_append counts them).  ctx_lens
+ * NULL: all 0.  A request whose ctx_lens is out of range keeps its rows
+ * (ENT_DEV_BAD_CTXLEN).
  * q, k: T rows of H_q d and H_kv d values with strides ldq, ldk (as for
  * ent_prompt_attention); q_out, k_out likewise.  An output may be its own input
  * (same pointer and stride); otherwise outputs must not overlap inputs or each

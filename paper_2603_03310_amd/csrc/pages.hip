@@ -465,7 +465,7 @@ __global__ __launch_bounds__(kPlanThreads) void release_kernel(ReleaseArgs a) {
 // release): -1 for every block in the first launch, and in the second one more for each
 // entry at its block's new place, and 0 for the free (10.4 us with 53 moves as without;
 // 1004 sequences, 251 holders a block, 237 us, 190 without).  Bound by the copies: 5120
-// moved blocks of 64 KB and their mean keys (713 MB) in 126 us of 137 = 5.7 TB/s, over a
+// moved blocks of 64 KB and their mean keys (713 MB) in 127 us of 137 = 5.6 TB/s, over a
 // large copy's 4.7; the first launch's 11 are the chain of round trips and 5 for the lists
 // of moves.  (One workgroup for a block, keys before values, four pieces a thread: 196 us
 // in all; through the caches 157.)
